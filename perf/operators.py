@@ -168,7 +168,7 @@ def _exponent(amax):
     """Byte of the power-of-two scale of a block whose largest magnitude is amax: the smallest with amax <= 448 * 2^e."""
     bits = amax.view(torch.int32)
     e = ((bits >> 23) & 255) - 8 + ((bits & 0x7FFFFF) > 0x600000).to(torch.int32)
-    return e.clamp(1, 254)
+    return e.clamp(16, 254)                       # what is far below 2^-111 is held as a part of that
 
 
 def _power(byte):
@@ -347,9 +347,9 @@ def _exact_mx8(x):
     """The values that an 8-bit cache holds of x [..., dim], in 64 bits."""
     b = x.reshape(*x.shape[:-1], -1, 32)
     amax = b.abs().amax(-1, keepdim=True)
-    e = torch.ceil(torch.log2(amax / 448.0).clamp(min=-126.0))
+    e = torch.ceil(torch.log2(amax / 448.0).clamp(min=-111.0))
     e = torch.where(amax > 448.0 * torch.exp2(e), e + 1, e)                 # log2 next to a whole number
-    e = torch.where((amax <= 448.0 * torch.exp2(e - 1)) & (e > -126), e - 1, e)
+    e = torch.where((amax <= 448.0 * torch.exp2(e - 1)) & (e > -111), e - 1, e)
     y = b * torch.exp2(-e)
     step = torch.exp2(torch.floor(torch.log2(y.abs().clamp(min=2.0 ** -6))) - 3)
     return (torch.round(y / step) * step * torch.exp2(e)).reshape(x.shape)
