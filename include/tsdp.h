@@ -260,6 +260,85 @@ int tsdp_kernel_ms(tsdp_ctx* ctx, int stage, float* h_ms);
  * workgroup per tile (compiled shapes), or instead of one launch per operator (others); the name stays the same. */
 const char* tsdp_path_name(const tsdp_ctx* ctx, int which);
 
+/* ---- Attention over observation histories ------------------------------------------------------------------------
+ *
+ * What makes the observation tokens that tsdp_set_cond takes: attention over whole prompts (the first observations of an
+ * episode, or a chunk of them behind its history), a paged cache of their keys / values, and attention of new tokens over
+ * that cache.  These calls use nothing of the context but its device, its error message and its status word, and no
+ * memory but the caller's: the context's device must be current (TSDP_E_STATE otherwise), nothing is allocated, no call
+ * synchronises, all can be captured in a HIP graph, and calls on different streams may overlap as long as their outputs and
+ * scratch are different memory.
+ *
+ * Packed rows: environment b owns rows ptr[b] .. ptr[b+1]-1 of its [rows, heads, head_dim] tensors (heads next to each
+ * other; *_row is the distance from one row to the next in elements, so a slice of a wider projection can be passed).  The
+ * live row count ptr[B] is read on the device; the *_cap arguments bound the launch and every access.  Rows and pools
+ * start at multiples of 16 bytes and rows are a multiple of 16 bytes apart, at most 2^24 elements.  Rows that no
+ * environment owns are neither read nor written.  head_dim is 32, 64 or 128.
+ *
+ * Keys that a query sees: with causal = 0 all of its environment's; with causal = 1 those up to its own place, the last
+ * query standing at the last key (query i of nq sees keys 0 .. nk - nq + i).  A query that sees no key gets zeros and a
+ * log-sum of -infinity.  Keys and values that a query does not see do not reach its result, whatever they hold (NaN,
+ * infinities, memory never written); a value it sees that is not finite gives NaN or infinity.  A query's result depends on
+ * its own environment's rows alone, bit for bit, not on the batch around it.
+ *
+ * log-sums (d_lse, optional): log sum_j exp(scale <q_i, k_j>), fp32 [query rows, q_heads].
+ *
+ * Status bits (tsdp_status): bit 5 = a row table or a length reached beyond its bound (clipped), bit 6 = a position or a page
+ * index outside the cache (not written; read as zeros; not attended to). */
+typedef struct {
+  int32_t type;           /* of queries, keys, values and outputs: 0 = fp32, 1 = bf16 */
+  int32_t q_heads, kv_heads, head_dim;   /* q_heads a multiple of kv_heads (at most 1024): query head h reads kv head h / (q_heads / kv_heads) */
+  int32_t causal;         /* 0 or 1 */
+  float   scale;          /* of the scores, > 0; usually 1 / sqrt(head_dim) */
+} tsdp_heads;
+
+/* A cache of keys / values in pages, all memory the caller's.  Pools are [pages, kv_heads, page_tokens, head_dim]; the token at
+ * position p of environment b lies in page page_table[b, p / page_tokens] at place p mod page_tokens.  Environments may share
+ * pages.  type 2 holds 8 bits: blocks of 32 elements along a head share one power of two, the smallest 2^e >= 2^-111 with
+ * max|x| <= 448 * 2^e (scale pools [pages, kv_heads, page_tokens, head_dim / 32] hold e + 127), and their elements are
+ * e4m3 of x * 2^-e, rounded to the nearest, ties to even; what is not finite is held as NaN.  A cache of bf16 takes fp32 rows
+ * rounded to the nearest, ties to even. */
+typedef struct {
+  int32_t type;           /* what is held: 0 = fp32, 1 = bf16, 2 = 8 bits */
+  int32_t kv_heads, head_dim;
+  int32_t page_tokens;    /* a power of two, 16..4096 */
+  int32_t pages;          /* in the pools */
+  int32_t B, columns;     /* of the page table */
+  void *d_k, *d_v;
+  uint8_t *d_k_scale, *d_v_scale;   /* type 2 only */
+  const int32_t* d_page_table;      /* [B, columns] */
+} tsdp_kv_cache;
+
+/* Writes the rows of new tokens into the cache: row i of environment b goes to position start[b] + i - row_ptr[b].  type: of the
+ * rows, 0 = fp32, 1 = bf16.  Two rows of a call must not go to the same place of the same page. */
+int tsdp_cache_write(tsdp_ctx* ctx, const tsdp_kv_cache* cache, int B, int R_cap, int type, const int32_t* d_row_ptr,
+                     const int32_t* d_start, const void* d_k, int64_t k_row, const void* d_v, int64_t v_row, void* stream);
+
+/* Reads them back as packed rows of fp32 (type 0) or bf16 (type 1): the keys / values of tsdp_attend_prompt for a chunk of
+ * tokens behind its history.  Values of 8 bits are exact in both types; fp32 ones are rounded to bf16 where that is asked for. */
+int tsdp_cache_read(tsdp_ctx* ctx, const tsdp_kv_cache* cache, int B, int R_cap, int type, const int32_t* d_row_ptr,
+                    const int32_t* d_start, void* d_k, int64_t k_row, void* d_v, int64_t v_row, void* stream);
+
+/* Attention of whole prompts.  d_q [q_cap, q_heads, head_dim] with d_q_ptr[B+1], d_k / d_v [k_cap, kv_heads, head_dim] with
+ * d_k_ptr[B+1] (NULL: as the queries, and k_cap = q_cap).  out: d_out as d_q.  Scores, sums and outputs are accumulated in
+ * fp32; with type 1 the weights are rounded to bf16 for their product with the values. */
+int tsdp_attend_prompt(tsdp_ctx* ctx, const tsdp_heads* heads, int B, int q_cap, int k_cap, const int32_t* d_q_ptr,
+                       const int32_t* d_k_ptr, const void* d_q, int64_t q_row, const void* d_k, int64_t k_row,
+                       const void* d_v, int64_t v_row, void* d_out, int64_t out_row, float* d_lse, void* stream);
+
+/* Attention of `tokens` (1..1024) new tokens of each of B environments over its first len[b] cached tokens, its own included:
+ * one token of a control step, the tokens of a new observation (causal), or queries that pool a history (causal = 0).
+ * d_q is [B * tokens, q_heads, head_dim] (type of the cache, or any with a cache of 8 bits); d_out is of out_type, 0 = fp32 or
+ * the type of d_q: fp32 outputs of cond_tokens queries with q_heads * head_dim = cond_dim are the d_cond of tsdp_set_cond.
+ * max_len bounds the lengths (a longer one is clipped to it) and with them the launch; long sequences are split into chunks
+ * whose results meet in d_scratch (tsdp_attend_scratch bytes, no initial contents needed). */
+int tsdp_attend_paged(tsdp_ctx* ctx, const tsdp_heads* heads, const tsdp_kv_cache* cache, int B, int tokens, int max_len,
+                      const int32_t* d_len, const void* d_q, int64_t q_row, int out_type, void* d_out, int64_t out_row,
+                      float* d_lse, void* d_scratch, int64_t scratch, void* stream);
+
+/* Bytes of scratch that such a call needs (0: none, d_scratch may be NULL), or a negative TSDP_E_* code. */
+int64_t tsdp_attend_scratch(const tsdp_heads* heads, int B, int tokens, int max_len);
+
 const char* tsdp_last_error(const tsdp_ctx* ctx);
 
 #ifdef __cplusplus

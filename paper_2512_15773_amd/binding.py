@@ -20,6 +20,7 @@ EXPORTS = ["tsdp_create", "tsdp_destroy", "tsdp_load_weights", "tsdp_set_cond", 
            "tsdp_accept", "tsdp_round", "tsdp_accept_threshold", "tsdp_round_threshold", "tsdp_chain", "tsdp_chain_staged",
            "tsdp_chain_enqueue", "tsdp_prepare",
            "tsdp_distill_loss", "tsdp_distill_loss_noalloc", "tsdp_status", "tsdp_kernel_timing", "tsdp_kernel_ms", "tsdp_path_name",
+           "tsdp_cache_write", "tsdp_cache_read", "tsdp_attend_prompt", "tsdp_attend_paged", "tsdp_attend_scratch",
            "tsdp_last_error"]
 
 
@@ -32,6 +33,17 @@ class TsdpConfig(C.Structure):
                 ("clip_x0", C.c_int32), ("clip_val", C.c_float), ("B_max", C.c_int32), ("K_max", C.c_int32),
                 ("seed", C.c_uint64), ("sampler", C.c_int32), ("eta", C.c_float),
                 ("bonus_row", C.c_int32), ("norm", C.c_int32)]
+
+
+class TsdpHeads(C.Structure):
+    _fields_ = [("type", C.c_int32), ("q_heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("causal", C.c_int32), ("scale", C.c_float)]
+
+
+class TsdpKvCache(C.Structure):
+    _fields_ = [("type", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("page_tokens", C.c_int32),
+                ("pages", C.c_int32), ("B", C.c_int32), ("columns", C.c_int32), ("d_k", C.c_void_p), ("d_v", C.c_void_p),
+                ("d_k_scale", C.c_void_p), ("d_v_scale", C.c_void_p), ("d_page_table", C.c_void_p)]
 
 
 _lib = None
@@ -66,6 +78,13 @@ def load_library():
     lib.tsdp_kernel_timing.argtypes = [vp, i32]
     lib.tsdp_kernel_ms.argtypes = [vp, i32, C.POINTER(C.c_float)]
     lib.tsdp_path_name.argtypes = [vp, i32]; lib.tsdp_path_name.restype = C.c_char_p
+    i64 = C.c_int64
+    lib.tsdp_cache_write.argtypes = [vp, C.POINTER(TsdpKvCache), i32, i32, i32, vp, vp, vp, i64, vp, i64, vp]
+    lib.tsdp_cache_read.argtypes = lib.tsdp_cache_write.argtypes
+    lib.tsdp_attend_prompt.argtypes = [vp, C.POINTER(TsdpHeads), i32, i32, i32, vp, vp] + [vp, i64] * 4 + [vp, vp]
+    lib.tsdp_attend_paged.argtypes = [vp, C.POINTER(TsdpHeads), C.POINTER(TsdpKvCache), i32, i32, i32, vp, vp, i64, i32, vp, i64, vp,
+                                      vp, i64, vp]
+    lib.tsdp_attend_scratch.argtypes = [C.POINTER(TsdpHeads), i32, i32, i32]; lib.tsdp_attend_scratch.restype = i64
     lib.tsdp_last_error.argtypes = [vp]; lib.tsdp_last_error.restype = C.c_char_p
     for name in EXPORTS:
         if getattr(lib, name).restype is C.c_int:
@@ -92,6 +111,49 @@ def _ptr(t, dtype=None):
 def _stream(stream):
     s = torch.cuda.current_stream() if stream is None else stream
     return s.cuda_stream
+
+
+_TYPE = {torch.float32: 0, torch.bfloat16: 1}
+
+
+def _rows(t, heads, dim, dtype, dev):
+    """Pointer and row stride of packed rows [rows, heads, dim]; the rows may be slices of wider ones."""
+    assert t.get_device() == dev, "packed rows must be on the current device"
+    assert t.dtype == dtype, f"expected {dtype}, got {t.dtype}"
+    assert t.dim() == 3 and t.shape[1:] == (heads, dim), f"expected [rows, {heads}, {dim}], got {tuple(t.shape)}"
+    rows, row = t.shape[0], t.stride(0)
+    if rows <= 1 or t.numel() == 0:
+        row = heads * dim
+    assert t.stride(2) == 1 and (heads == 1 or t.stride(1) == dim), "the heads of a row must be next to each other"
+    return t.data_ptr(), row
+
+
+class KvCache:
+    """A paged cache of keys / values (tsdp_kv_cache): pools k, v [pages, kv_heads, page_tokens, head_dim] in float32, bfloat16
+    or uint8 (8 bits, with scale pools [pages, kv_heads, page_tokens, head_dim // 32] in uint8) and the int32 page table
+    [B, columns].  The tensors are the caller's and stay the cache's memory: change the table in place."""
+
+    def __init__(self, k, v, page_table, k_scale=None, v_scale=None):
+        held = {**_TYPE, torch.uint8: 2}
+        assert k.dtype in held, f"a cache holds float32, bfloat16 or uint8, not {k.dtype}"
+        assert k.dim() == 4 and k.shape == v.shape and k.dtype == v.dtype, "k and v must be alike, [pages, kv_heads, page_tokens, head_dim]"
+        assert page_table.dim() == 2 and k.get_device() == v.get_device() == page_table.get_device(), "pools and table must be on one device"
+        pages, kv, page, dim = k.shape
+        assert (k_scale is None) == (v_scale is None) == (held[k.dtype] != 2), "scale pools belong to 8 bits, and to nothing else"
+        for s in (k_scale, v_scale):
+            assert s is None or (tuple(s.shape) == (pages, kv, page, dim // 32) and s.get_device() == k.get_device()), "scale pools must be [pages, kv_heads, page_tokens, head_dim // 32]"
+        self.k, self.v, self.k_scale, self.v_scale, self.page_table = k, v, k_scale, v_scale, page_table
+        self.kv_heads, self.head_dim, self.device, self.B = kv, dim, k.get_device(), page_table.shape[0]
+        self.c = TsdpKvCache(type=held[k.dtype], kv_heads=kv, head_dim=dim, page_tokens=page, pages=pages, B=page_table.shape[0],
+                             columns=page_table.shape[1], d_k=_ptr(k), d_v=_ptr(v), d_k_scale=_ptr(k_scale, torch.uint8),
+                             d_v_scale=_ptr(v_scale, torch.uint8), d_page_table=_ptr(page_table, torch.int32))
+
+    @classmethod
+    def alloc(cls, dtype, pages, kv_heads, page_tokens, head_dim, page_table):
+        """Pools of zeros; dtype float32, bfloat16, or uint8 for 8 bits."""
+        f = lambda d, dt: torch.zeros(pages, kv_heads, page_tokens, d, dtype=dt, device=page_table.device)
+        scales = [f(head_dim // 32, torch.uint8) for _ in "kv"] if dtype == torch.uint8 else [None, None]
+        return cls(f(head_dim, dtype), f(head_dim, dtype), page_table, *scales)
 
 
 class Tsdp:
@@ -282,6 +344,83 @@ class Tsdp:
         self._chk(self.lib.tsdp_round(self.ctx, x.shape[0], _ptr(x, torch.float32), _ptr(t, torch.int32),
                                       _ptr(K, torch.int32), _ptr(sigma_scale, torch.float32), _ptr(env_id, torch.int32),
                                       _ptr(n_accept, torch.int32), _ptr(n_advanced, torch.int32), _stream(stream)))
+
+    def _cache_rows(self, call, cache, row_ptr, start, k, v, stream):
+        dev = torch.cuda.current_device()
+        assert cache.device == dev, "the cache must be on the current device"
+        kp, k_row = _rows(k, cache.kv_heads, cache.head_dim, k.dtype, dev)
+        vp, v_row = _rows(v, cache.kv_heads, cache.head_dim, k.dtype, dev)
+        assert k.dtype in _TYPE and k.shape[0] == v.shape[0], "rows of keys and values must be alike, float32 or bfloat16"
+        assert row_ptr.shape[0] == start.shape[0] + 1, "row_ptr has one entry more than start"
+        self._chk(call(self.ctx, cache.c, start.shape[0], k.shape[0], _TYPE[k.dtype], _ptr(row_ptr, torch.int32), _ptr(start, torch.int32),
+                       kp, k_row, vp, v_row, _stream(stream)))
+
+    def tsdp_cache_write(self, cache, row_ptr, start, k, v, stream=None):
+        """Rows row_ptr[b] .. of k, v [rows, kv_heads, head_dim] to positions start[b] .. of environment b."""
+        self._cache_rows(self.lib.tsdp_cache_write, cache, row_ptr, start, k, v, stream)
+
+    def tsdp_cache_read(self, cache, row_ptr, start, rows, dtype, out=None, stream=None):
+        """Positions start[b] .. of every environment as packed rows (k, v); out: such a pair to write into."""
+        if out is None:
+            out = tuple(torch.empty(rows, cache.kv_heads, cache.head_dim, dtype=dtype, device=row_ptr.device) for _ in "kv")
+        assert out[0].dtype == dtype and out[0].shape[0] == rows, "out must hold `rows` rows of the given type"
+        self._cache_rows(self.lib.tsdp_cache_read, cache, row_ptr, start, out[0], out[1], stream)
+        return out
+
+    @staticmethod
+    def _lse(lse, rows, heads, dev):
+        assert lse is None or (tuple(lse.shape) == (rows, heads) and lse.get_device() == dev), f"lse must be [{rows}, {heads}]"
+        return _ptr(lse, torch.float32)
+
+    def tsdp_attend_prompt(self, q, k, v, q_ptr, k_ptr=None, *, causal=True, scale=None, out=None, lse=None, stream=None):
+        """q [rows, q_heads, head_dim] (float32 or bfloat16), k, v [rows of keys, kv_heads, head_dim]; returns out."""
+        dev = torch.cuda.current_device()
+        heads, dim, kv = q.shape[1], q.shape[2], k.shape[1]
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        qp, q_row = _rows(q, heads, dim, q.dtype, dev)
+        kp, k_row = _rows(k, kv, dim, q.dtype, dev)
+        vp, v_row = _rows(v, kv, dim, q.dtype, dev)
+        op, out_row = _rows(out, heads, dim, q.dtype, dev)
+        assert q.dtype in _TYPE and out.shape == q.shape and v.shape[0] == k.shape[0], "q and out, k and v must be alike, float32 or bfloat16"
+        assert k_ptr is None or k_ptr.shape == q_ptr.shape, "q_ptr and k_ptr must be of one length"
+        h = TsdpHeads(_TYPE[q.dtype], heads, kv, dim, 1 if causal else 0, dim ** -0.5 if scale is None else scale)
+        self._chk(self.lib.tsdp_attend_prompt(self.ctx, h, q_ptr.shape[0] - 1, q.shape[0], k.shape[0], _ptr(q_ptr, torch.int32),
+                                              _ptr(k_ptr, torch.int32), qp, q_row, kp, k_row, vp, v_row, op, out_row,
+                                              self._lse(lse, q.shape[0], heads, dev), _stream(stream)))
+        return out
+
+    def alloc_scratch(self, cache, q_heads, tokens, max_len, B=None):
+        """Scratch of tsdp_attend_paged for B environments (default: as many as the page table has), uint8, or None."""
+        h = TsdpHeads(0, q_heads, cache.kv_heads, cache.head_dim, 1, 1.0)
+        n = self.lib.tsdp_attend_scratch(h, cache.B if B is None else B, tokens, max_len)
+        if n < 0:
+            raise TsdpError(int(n), "tsdp_attend_scratch rejected the sizes")
+        return torch.empty(n, dtype=torch.uint8, device=cache.k.device) if n else None
+
+    def tsdp_attend_paged(self, q, cache, length, max_len, *, tokens=1, causal=True, scale=None, out_dtype=None, out=None, lse=None,
+                          scratch=None, stream=None):
+        """q [B * tokens, q_heads, head_dim] over the first length[b] tokens of the cache; returns out (out_dtype: float32 or
+        that of q).  scratch: from alloc_scratch (allocated for the call where it is left out)."""
+        dev = torch.cuda.current_device()
+        assert cache.device == dev and length.get_device() == dev, "cache and lengths must be on the current device"
+        rows, heads, dim = q.shape
+        B = length.shape[0]
+        assert q.dtype in _TYPE and rows == B * tokens and dim == cache.head_dim, "q must be [B * tokens, q_heads, head_dim], float32 or bfloat16"
+        if out is None:
+            out = torch.empty(q.shape, dtype=out_dtype or q.dtype, device=q.device)
+        assert out.dtype in _TYPE and out.shape == q.shape and out_dtype in (None, out.dtype), "out must be alike q, float32 or bfloat16"
+        if scratch is None:
+            scratch = self.alloc_scratch(cache, heads, tokens, max_len, B)
+            if scratch is not None and stream is not None:
+                scratch.record_stream(stream)
+        qp, q_row = _rows(q, heads, dim, q.dtype, dev)
+        op, out_row = _rows(out, heads, dim, out.dtype, dev)
+        h = TsdpHeads(_TYPE[q.dtype], heads, cache.kv_heads, dim, 1 if causal else 0, dim ** -0.5 if scale is None else scale)
+        self._chk(self.lib.tsdp_attend_paged(self.ctx, h, cache.c, B, tokens, max_len, _ptr(length, torch.int32), qp, q_row,
+                                             _TYPE[out.dtype], op, out_row, self._lse(lse, rows, heads, dev), _ptr(scratch),
+                                             0 if scratch is None else scratch.numel() * scratch.element_size(), _stream(stream)))
+        return out
 
     def tsdp_kernel_timing(self, enable):
         """False / 0 = off, True / 1 = all stages, 2 * mask = chosen stages (mask bit 0 drafter, 1 verify, 2 accept)."""

@@ -1,0 +1,412 @@
+// Attention of new tokens over the paged cache, split over the cache's length and joined.
+//
+// Bound by the stream of keys and values out of HBM: every byte is loaded once per 16 columns (queries x heads of a group),
+// straight from the pages into registers.  A workgroup takes one chunk of one environment's sequence and one kv head; its
+// four waves take 32 keys at a time, each with a running softmax of its own, and join through LDS.  A sequence of more than
+// one chunk leaves (output, maximum, sum) per chunk in the scratch, which k_paged_join adds up in the order of the chunks.
+//
+// As in the prompt kernels both products are transposed.  S^T = K Q^T with 16 keys x 16 columns; the score registers of the
+// two halves of a tile are keys 4 g + i and 16 + 4 g + i of lane group g = l / 16, which is the operand of P^T as it is
+// when the value operand takes its keys in that order.  A lane loads D / 16 neighbouring values of those eight keys (whole
+// rows per 16 lanes) and turns them with byte permutes into D / 16 operands, operand f holding dims (D / 16) r + f.
+//
+// Fewer than 32 bits enter a matrix product only without loss: keys and values as they are held (8 bits widen exactly to
+// bf16 with their scale), fp32 queries as three bf16 parts, and the weights P as two or three (to 2^-16 or 2^-24 of each).
+#pragma once
+#include "attend_common.hpp"
+
+namespace tsdp {
+
+struct PagedArgs {
+  CacheView cache;
+  int B, heads, tokens, cols, max_len, max_chunks, causal;   // cols = tokens * heads / kv_heads
+  float c;
+  const int32_t* len;
+  const void* q; void* out;
+  int64_t q_row, out_row;
+  float* lse;                                // [B * tokens][heads] or null
+  float* part;                               // scratch: [B][kv][cols][max_chunks][D], then as many (maximum, sum)
+  float* part_ml;
+  int32_t* status;
+};
+
+__device__ __forceinline__ int paged_len(const PagedArgs& a, int b) {
+  const long room = min((long)a.max_len, (long)a.cache.columns << a.cache.page_shift);
+  const int n = a.len[b];
+  if (n > room && threadIdx.x == 0) report(a.status, STATUS_ROWS);
+  return n < 0 ? 0 : (int)min((long)n, room);
+}
+
+template <int D, int HELD> struct PagedTile;
+
+template <int D> struct PagedTile<D, HELD_BF16> {
+  u32x4 k[2][D / 32];
+  uint32_t v[8][D / 32];
+  static constexpr int q_dim(int ks, int g) { return 32 * ks + 8 * g; }   // first of the 8 dims of lane group g in k-step ks
+  __device__ __forceinline__ void load(const CacheView& c, const int64_t* row, int lane) {
+    const int r = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const uint8_t* kp = static_cast<const uint8_t*>(c.k) + row[s] * (2 * D) + r * (2 * D) + g * 16;
+#pragma unroll
+      for (int x = 0; x < D / 32; ++x) k[s][x] = *reinterpret_cast<const u32x4*>(kp + 64 * x);
+      const uint8_t* vp = static_cast<const uint8_t*>(c.v) + row[s] * (2 * D) + (4 * g) * (2 * D) + r * (D / 8);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) __builtin_memcpy(v[4 * s + i], __builtin_assume_aligned(vp + i * (2 * D), D / 8), D / 8);
+    }
+  }
+  __device__ __forceinline__ bf16x8 key(int s, int ks, int) const { return __builtin_bit_cast(bf16x8, k[s][ks]); }
+  __device__ __forceinline__ void values(uint32_t (&w)[8][D / 32], int) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int x = 0; x < D / 32; ++x) w[i][x] = v[i][x];
+  }
+};
+
+template <int D> struct PagedTile<D, HELD_MX8> {
+  static constexpr int NB = D / MX_BLOCK, KV = D >= 64 ? D / 64 : 1;      // scales a row, key loads a row
+  static constexpr int KW = D >= 64 ? 4 : 2;                              // words of a key load
+  uint32_t k[2][KV][KW], ks[2];
+  uint32_t v[8][D / 64 ? D / 64 : 1], vs[2][NB];                          // D = 32: two values a key, in the low half
+  static constexpr int q_dim(int s, int g) { return D >= 64 ? 64 * (s / 2) + 16 * g + 8 * (s % 2) : 8 * g; }
+  __device__ __forceinline__ void load(const CacheView& c, const int64_t* row, int lane) {
+    const int r = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const uint8_t* kp = static_cast<const uint8_t*>(c.k) + (row[s] + r) * D + g * (4 * KW);
+#pragma unroll
+      for (int x = 0; x < KV; ++x) __builtin_memcpy(k[s][x], __builtin_assume_aligned(kp + 64 * x, 4 * KW), 4 * KW);
+      ks[s] = 0;
+      __builtin_memcpy(&ks[s], __builtin_assume_aligned(c.k_scale + (row[s] + r) * NB, NB), NB);
+      const uint8_t* vp = static_cast<const uint8_t*>(c.v) + (row[s] + 4 * g) * D + r * (D / 16);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[4 * s + i][0] = 0;
+        __builtin_memcpy(v[4 * s + i], __builtin_assume_aligned(vp + i * D, D / 16), D / 16);
+      }
+      __builtin_memcpy(vs[s], __builtin_assume_aligned(c.v_scale + (row[s] + 4 * g) * NB, 4 * NB), 4 * NB);
+    }
+  }
+  __device__ __forceinline__ bf16x8 key(int s, int x, int lane) const {
+    const int g = lane >> 4;
+    const float f = D >= 64 ? scale_of((ks[s] >> (8 * (2 * (x / 2) + g / 2))) & 255) : scale_of(ks[s] & 255);
+    const int at = D >= 64 ? 2 * (x % 2) : 0;
+    const u32x2 lo = mx8_to_bf16(k[s][x / 2][at], f), hi = mx8_to_bf16(k[s][x / 2][at + 1], f);
+    return __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
+  }
+  __device__ __forceinline__ void values(uint32_t (&w)[8][D / 32], int lane) const {
+    const int r = lane & 15;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      // byte of key i % 4's scale of the block that dims (D / 16) r .. lie in
+      const int block = r * (D / 16) / MX_BLOCK, byte = (i % 4) * NB;
+      const uint32_t word = D == 128 ? vs[i / 4][i % 4] : D == 64 ? vs[i / 4][(i % 4) / 2] : vs[i / 4][0];
+      const float f = scale_of((word >> (8 * (byte % 4 + block))) & 255);
+      if constexpr (D == 32) {
+        w[i][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[i][0], f, false));
+      } else {
+#pragma unroll
+        for (int x = 0; x < D / 64; ++x) {
+          const u32x2 y = mx8_to_bf16(v[i][x], f);
+          w[i][2 * x] = y[0]; w[i][2 * x + 1] = y[1];
+        }
+      }
+    }
+  }
+};
+
+template <int D> struct PagedTile<D, HELD_F32> {
+  f32x4 k[2][D / 16];
+  float v[8][D / 16];
+  __device__ __forceinline__ void load(const CacheView& c, const int64_t* row, int lane) {
+    const int r = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const float* kp = static_cast<const float*>(c.k) + (row[s] + r) * D + g * 4;
+#pragma unroll
+      for (int x = 0; x < D / 16; ++x) k[s][x] = *reinterpret_cast<const f32x4*>(kp + 16 * x);
+      const float* vp = static_cast<const float*>(c.v) + (row[s] + 4 * g) * D + r * (D / 16);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        __builtin_memcpy(v[4 * s + i], __builtin_assume_aligned(vp + i * D, D / 4 < 16 ? D / 4 : 16), D / 4);
+    }
+  }
+};
+
+// x as NP bf16 parts whose sum it is to 2^-8 (1), 2^-16 (2), 2^-24 (3) of it
+template <int NP>
+__device__ __forceinline__ void split(float x, __bf16 (&p)[NP]) {
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    p[i] = (__bf16)x;
+    x = not_finite_f32(x) ? 0.f : x - (float)p[i];
+  }
+}
+
+// QF32: queries are fp32.  NP: bf16 parts of P (unused where the cache is fp32).
+template <int D, int HELD, bool QF32, int NP, typename Out>
+__global__ __launch_bounds__(256) void k_paged(PagedArgs a) {
+  constexpr bool F32 = HELD == HELD_F32;
+  constexpr int NQ = QF32 && !F32 ? 3 : 1, F = D / 16, OP = D + 4;
+  __shared__ __align__(16) float o_lds[4][16][OP];
+  __shared__ float ml_lds[4][16][2];
+  const int kv = a.cache.kv_heads, ct = (a.cols + 15) / 16;
+  const int kvh = blockIdx.x % kv, rest = blockIdx.x / kv, col0 = (rest % ct) * 16, b = rest / ct, chunk = blockIdx.y;
+  const int len = paged_len(a, b);
+  const int shift = chunk_shift(len, a.cols), chunks = chunks_of(len, a.cols);
+  if (chunk > 0 && chunk >= chunks) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+  const int G = a.heads / kv, col = col0 + r, at = min(col, a.cols - 1);
+  const int token = at / G, head = kvh * G + at % G;
+  const int mine = col < a.cols ? seen(token, a.tokens, len, a.causal) : 0;
+  const int all = seen(col0 / G, a.tokens, len, a.causal);       // keys that every column of the tile sees
+
+  const int64_t q_at = ((int64_t)b * a.tokens + token) * a.q_row + head * D;
+  bf16x8 qf[NQ][D / 32];
+  f32x4 qx[F];
+  if constexpr (F32) {
+#pragma unroll
+    for (int x = 0; x < F; ++x) qx[x] = *reinterpret_cast<const f32x4*>(static_cast<const float*>(a.q) + q_at + 16 * x + 4 * g);
+  } else {
+#pragma unroll
+    for (int x = 0; x < D / 32; ++x) {
+      const int d = PagedTile<D, HELD>::q_dim(x, g);
+      if constexpr (QF32) {
+        const float* p = static_cast<const float*>(a.q) + q_at + d;
+#pragma unroll
+        for (int y = 0; y < 8; ++y) {
+          __bf16 parts[3];
+          split<3>(p[y], parts);
+#pragma unroll
+          for (int z = 0; z < 3; ++z) qf[z][x][y] = parts[z];
+        }
+      } else {
+        qf[0][x] = *reinterpret_cast<const bf16x8*>(static_cast<const __bf16*>(a.q) + q_at + d);
+      }
+    }
+  }
+
+  f32x4 o[F];
+#pragma unroll
+  for (int f = 0; f < F; ++f) o[f] = f32x4{};
+  float m = -INFINITY, l = 0.f;
+  const int per_wave = 1 << (shift - 2);                         // keys of a wave
+  const long lo = ((long)chunk << shift) + wave * per_wave, hi = min(lo + per_wave, (long)len);
+  for (long k0 = lo; k0 < hi; k0 += 32) {
+    int64_t row[2];
+    bool ok[2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {                                // 16 keys lie in one page
+      const long pos = k0 + 16 * s;
+      const int page = pos < len ? page_of(a.cache, b, pos >> a.cache.page_shift) : 0;
+      ok[s] = page >= 0;
+      if (!ok[s] && lane == 0) report(a.status, STATUS_PAGE);
+      row[s] = pool_row(a.cache, max(page, 0), kvh, (int)(pos & ((1L << a.cache.page_shift) - 1)));
+    }
+    PagedTile<D, HELD> t;
+    t.load(a.cache, row, lane);
+    f32x4 s[2] = {f32x4{}, f32x4{}};
+    if constexpr (F32) {
+#pragma unroll
+      for (int x = 0; x < F; ++x)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) s[u] = __builtin_amdgcn_mfma_f32_16x16x4f32(t.k[u][x][j], qx[x][j], s[u], 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int x = 0; x < D / 32; ++x)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const bf16x8 key = t.key(u, x, lane);
+#pragma unroll
+          for (int z = NQ - 1; z >= 0; --z) s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, qf[z][x], s[u], 0, 0, 0);
+        }
+    }
+    const bool masked = k0 + 32 > all || !ok[0] || !ok[1];
+    bool sees[8];
+    if (masked) {
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        sees[x] = ok[x / 4] && k0 + 16 * (x / 4) + 4 * g + x % 4 < mine;
+        if (!sees[x]) s[x / 4][x % 4] = -INFINITY;
+      }
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int x = 1; x < 8; ++x) top = fmaxf(top, s[x / 4][x % 4]);
+    top = max_groups(top) * a.c;
+    // the running maximum moves only where it would grow by more than 2^8
+    if (__any(top > m + 8.f)) {
+      const float to = top > m + 8.f ? top : m, f = to == m ? 1.f : __builtin_amdgcn_exp2f(m - to);   // each query by its own scores
+      m = to;
+      l *= f;
+#pragma unroll
+      for (int y = 0; y < F; ++y)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) o[y][x] *= f;
+    }
+    const float sub = m == -INFINITY ? 0.f : m;
+    float p[8];
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      p[x] = __builtin_amdgcn_exp2f(fmaf(s[x / 4][x % 4], a.c, -sub));
+      l += p[x];
+    }
+    if constexpr (F32) {
+      bool bad = false;
+      if (masked) {
+#pragma unroll
+        for (int x = 0; x < 8; ++x)
+#pragma unroll
+          for (int f = 0; f < F; ++f) bad |= not_finite_f32(t.v[x][f]);
+      }
+      if (masked && __any(bad)) {
+        // values that are not finite are taken out of the product, and set the outputs of the queries that see them
+#pragma unroll
+        for (int f = 0; f < F; ++f) {
+          f32x4 marks = f32x4{};
+#pragma unroll
+          for (int x = 0; x < 8; ++x) {
+            const bool n = not_finite_f32(t.v[x][f]);
+            o[f] = __builtin_amdgcn_mfma_f32_16x16x4f32(n ? 0.f : t.v[x][f], p[x], o[f], 0, 0, 0);
+            marks = __builtin_amdgcn_mfma_f32_16x16x4f32(n ? 1.f : 0.f, sees[x] ? 1.f : 0.f, marks, 0, 0, 0);
+          }
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            if (marks[x] != 0.f) o[f][x] = NAN;
+        }
+      } else {
+#pragma unroll
+        for (int x = 0; x < 8; ++x)
+#pragma unroll
+          for (int f = 0; f < F; ++f) o[f] = __builtin_amdgcn_mfma_f32_16x16x4f32(t.v[x][f], p[x], o[f], 0, 0, 0);
+      }
+    } else {
+      bf16x8 pf[NP];
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        __bf16 parts[NP];
+        split<NP>(p[x], parts);
+#pragma unroll
+        for (int z = 0; z < NP; ++z) pf[z][x] = parts[z];
+      }
+      uint32_t w[8][D / 32];
+      t.values(w, lane);
+      bool bad = false;
+      if (masked) {
+#pragma unroll
+        for (int x = 0; x < 8; ++x)
+#pragma unroll
+          for (int y = 0; y < D / 32; ++y) bad |= not_finite_bf16(w[x][y]);
+      }
+      const bool unusual = masked && __any(bad);
+#pragma unroll
+      for (int y = 0; y < D / 32; ++y)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {                            // low and high halves of the words: operand 2 y + h
+          u32x4 v;
+#pragma unroll
+          for (int x = 0; x < 4; ++x) v[x] = __builtin_amdgcn_perm(w[2 * x + 1][y], w[2 * x][y], h ? 0x07060302u : 0x05040100u);
+          const int f = 2 * y + h;
+          if (unusual) {
+            u32x4 mark;
+            bf16x8 one;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) { mark[x] = marks_bf16(v[x]); v[x] = finite_bf16(v[x]); }
+#pragma unroll
+            for (int x = 0; x < 8; ++x) one[x] = (__bf16)(sees[x] ? 1.f : 0.f);
+            const f32x4 marks = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, mark), one, f32x4{}, 0, 0, 0);
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+              if (marks[x] != 0.f) o[f][x] = NAN;
+          }
+#pragma unroll
+          for (int z = NP - 1; z >= 0; --z)
+            o[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), pf[z], o[f], 0, 0, 0);
+        }
+    }
+  }
+  l = sum_groups(l);
+  if (g == 0) { ml_lds[wave][r][0] = m; ml_lds[wave][r][1] = l; }
+#pragma unroll
+  for (int x = 0; x < 4; ++x)                                    // accumulator row 4 g + x of operand f: dim F (4 g + x) + f
+#pragma unroll
+    for (int f = 0; f < F; ++f) o_lds[wave][r][F * (4 * g + x) + f] = o[f][x];
+  __syncthreads();
+
+  const int c = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * F;   // 16 threads a column, D / 16 dims each
+  if (col0 + c >= a.cols) return;
+  float top = -INFINITY, total = 0.f, y[F];
+#pragma unroll
+  for (int w = 0; w < 4; ++w) top = fmaxf(top, ml_lds[w][c][0]);
+#pragma unroll
+  for (int f = 0; f < F; ++f) y[f] = 0.f;
+  const float sub = top == -INFINITY ? 0.f : top;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float f = __builtin_amdgcn_exp2f(ml_lds[w][c][0] - sub);
+    total = fmaf(ml_lds[w][c][1], f, total);
+#pragma unroll
+    for (int x = 0; x < F; ++x) y[x] = fmaf(o_lds[w][c][d0 + x], f, y[x]);
+  }
+  const int token_c = (col0 + c) / G, head_c = kvh * G + (col0 + c) % G;
+  if (chunks > 1) {
+    const int64_t at_c = (((int64_t)b * kv + kvh) * a.cols + col0 + c) * a.max_chunks + chunk;
+#pragma unroll
+    for (int x = 0; x < F; ++x) a.part[at_c * D + d0 + x] = y[x];
+    if (d0 == 0) { a.part_ml[2 * at_c] = top; a.part_ml[2 * at_c + 1] = total; }
+  } else {
+    const int64_t row = (int64_t)b * a.tokens + token_c;
+    Out* out = static_cast<Out*>(a.out) + row * a.out_row + head_c * D + d0;
+#pragma unroll
+    for (int x = 0; x < F; ++x) out[x] = (Out)(total == 0.f ? 0.f : y[x] / total);
+    if (a.lse && d0 == 0) a.lse[row * a.heads + head_c] = (top + __builtin_amdgcn_logf(total)) * LN2;
+  }
+}
+
+// One workgroup adds up the chunks of one column, each of its four waves every fourth one.
+template <int D, typename Out>
+__global__ __launch_bounds__(256) void k_paged_join(PagedArgs a) {
+  constexpr int E = D >= 64 ? D / 64 : 1;                        // dims of a lane
+  __shared__ float o_lds[4][D];
+  __shared__ float ml_lds[4];
+  const int col = blockIdx.x % a.cols, kvh = blockIdx.x / a.cols % a.cache.kv_heads, b = blockIdx.x / a.cols / a.cache.kv_heads;
+  const int len = paged_len(a, b), chunks = chunks_of(len, a.cols);
+  if (chunks <= 1) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, d0 = lane * E;
+  const int64_t at = (((int64_t)b * a.cache.kv_heads + kvh) * a.cols + col) * a.max_chunks;
+  const float* ml = a.part_ml + 2 * at;
+  float top = -INFINITY;
+  for (int n = lane; n < chunks; n += 64) top = fmaxf(top, ml[2 * n]);
+#pragma unroll
+  for (int s = 32; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor(top, s));
+  const float sub = top == -INFINITY ? 0.f : top;
+  float y[E], total = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) y[e] = 0.f;
+  for (int n = wave; n < chunks; n += 4) {
+    const float f = __builtin_amdgcn_exp2f(ml[2 * n] - sub);
+    total = fmaf(ml[2 * n + 1], f, total);
+    if (d0 < D) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) y[e] = fmaf(a.part[(at + n) * D + d0 + e], f, y[e]);
+    }
+  }
+  if (lane == 0) ml_lds[wave] = total;
+  if (d0 < D) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) o_lds[wave][d0 + e] = y[e];
+  }
+  __syncthreads();
+  if ((int)threadIdx.x >= D) return;
+  total = ml_lds[0] + ml_lds[1] + ml_lds[2] + ml_lds[3];
+  const float x = o_lds[0][threadIdx.x] + o_lds[1][threadIdx.x] + o_lds[2][threadIdx.x] + o_lds[3][threadIdx.x];
+  const int G = a.heads / a.cache.kv_heads, head = kvh * G + col % G;
+  const int64_t row = (int64_t)b * a.tokens + col / G;
+  static_cast<Out*>(a.out)[row * a.out_row + head * D + threadIdx.x] = (Out)(total == 0.f ? 0.f : x / total);
+  if (a.lse && threadIdx.x == 0) a.lse[row * a.heads + head] = (top + __builtin_amdgcn_logf(total)) * LN2;
+}
+
+}  // namespace tsdp

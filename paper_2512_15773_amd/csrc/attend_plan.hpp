@@ -1,0 +1,73 @@
+// Rules of attention and of the key / value cache that host and device share: which sequence a packed row belongs to,
+// where a token lies in the pages, how a length is split into chunks.  Plain C++: the CPU tests compile this file alone.
+#pragma once
+#include <stdint.h>
+
+#ifdef __HIPCC__
+#define TSDP_HD __host__ __device__ __forceinline__
+#else
+#define TSDP_HD inline
+#endif
+
+namespace tsdp {
+
+constexpr int MX_BLOCK = 32;                 // elements that share a scale in the 8-bit cache
+constexpr int MIN_PAGE_SHIFT = 4, MAX_PAGE_SHIFT = 12;
+
+struct CacheView {                           // tsdp_kv_cache, checked
+  void* k; void* v; uint8_t* k_scale; uint8_t* v_scale;
+  const int32_t* table;                      // [B][columns]
+  int32_t pages, columns, kv_heads, page_shift;
+};
+
+// Page of column `col` of environment b, -1 where the column or the table's entry lies outside (nothing is read through
+// such an entry).
+TSDP_HD int page_of(const CacheView& c, int b, long col) {
+  if (col < 0 || col >= c.columns) return -1;
+  const int32_t p = c.table[(long)b * c.columns + col];
+  return p < 0 || p >= c.pages ? -1 : p;
+}
+
+// Row of `token` (its place in the page) of a head in the pools, counted in rows of head_dim elements: past 32 bits in
+// a long cache.
+TSDP_HD int64_t pool_row(const CacheView& c, int page, int head, int token) {
+  return ((((int64_t)page * c.kv_heads + head) << c.page_shift) + token);
+}
+
+// Live rows b .. of a packed table: [lo, hi) clipped to 0 .. cap; an entry that points backwards owns no rows.
+TSDP_HD void rows_of(const int32_t* ptr, int b, int cap, int& lo, int& hi) {
+  lo = ptr[b]; hi = ptr[b + 1];
+  if (lo < 0 || lo > cap) { lo = 0; hi = 0; }
+  if (hi > cap) hi = cap;
+  if (hi < lo) hi = lo;
+}
+
+// Keys that query i of nq sees of nk: all, or (causal) those up to its own place, the last query at the last key.
+TSDP_HD int seen(int i, int nq, int nk, bool causal) {
+  if (!causal) return nk;
+  const long n = (long)nk - nq + 1 + i;
+  return n < 0 ? 0 : n > nk ? nk : (int)n;
+}
+
+// Chunk of a sequence that one workgroup of the paged kernel takes, from the sequence's own length and the columns
+// (queries x heads of a group) alone, so that a result does not depend on the batch around it.
+TSDP_HD int chunk_shift(int len, int cols) {
+  int s = cols <= 16 ? 8 : cols <= 32 ? 9 : cols <= 64 ? 10 : 11;
+  if (len > (1 << 14) && s < 10) s = 10;
+  return s;
+}
+TSDP_HD int chunks_of(int len, int cols) {
+  const int s = chunk_shift(len, cols);
+  return (int)(((long)len + (1L << s) - 1) >> s);
+}
+// the most chunks that a length of at most max_len has
+inline int most_chunks(int max_len, int cols) {
+  int n = chunks_of(max_len, cols);
+  if (max_len > (1 << 14)) {
+    const int below = chunks_of(1 << 14, cols);
+    if (below > n) n = below;
+  }
+  return n;
+}
+
+}  // namespace tsdp

@@ -19,6 +19,7 @@
 #include "row_dyn.hpp"
 #include "flow_rows.hpp"
 #include "round_kernels.hpp"
+#include "ctx_access.hpp"
 
 using namespace tsdp;
 
@@ -985,6 +986,18 @@ int check_ready(tsdp_ctx* c, int B, bool need_nets) {
 }
 
 }  // namespace
+
+namespace tsdp {
+int ctx_fail(tsdp_ctx* c, int code, const char* msg) noexcept {
+  try {
+    c->err = msg;
+  } catch (...) {                 // no memory for the message: the code alone
+  }
+  return code;
+}
+int ctx_device(const tsdp_ctx* c) noexcept { return c->device; }
+int32_t* ctx_status(tsdp_ctx* c) noexcept { return c->status; }
+}  // namespace tsdp
 
 extern "C" {
 
