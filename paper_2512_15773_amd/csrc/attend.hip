@@ -66,14 +66,21 @@ int cache_rows(tsdp_ctx* c, const tsdp_kv_cache* cache, int B, int R_cap, int ty
   return launched(c);
 }
 
+template <int TQ>
+dim3 prompt_grid(PromptArgs& a) {
+  a.slots = a.q_cap / TQ + a.B;
+  return dim3((unsigned)((int64_t)a.slots * a.heads));
+}
+
 template <int D>
-void launch_prompt(int type, const PromptArgs& in, hipStream_t s) {
-  constexpr int NW = 4;
-  PromptArgs a = in;
-  a.slots = a.q_cap / (32 * NW) + a.B;
-  const dim3 grid((unsigned)((int64_t)a.slots * a.heads));
-  if (type == 0) hipLaunchKernelGGL((k_prompt_f32<D, NW>), grid, dim3(NW * 64), 0, s, a);
-  else hipLaunchKernelGGL((k_prompt_bf16<D, NW>), grid, dim3(NW * 64), 0, s, a);
+void launch_prompt(int type, PromptArgs a, hipStream_t s) {
+  if (type == 0) {
+    const dim3 grid = prompt_grid<128>(a);
+    hipLaunchKernelGGL((k_prompt_f32<D, 4>), grid, dim3(256), 0, s, a);
+  } else {
+    const dim3 grid = prompt_grid<128>(a);
+    hipLaunchKernelGGL((k_prompt_bf16<D, 4, 2>), grid, dim3(256), 0, s, a);
+  }
 }
 
 template <int D, int HELD, bool QF32, int NP, typename Out>

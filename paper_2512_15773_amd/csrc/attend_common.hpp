@@ -46,10 +46,14 @@ __device__ __forceinline__ u32x2 mx8_to_bf16(uint32_t w, float scale) {
   return r;
 }
 
+// NaN where one of them is (v_maximum3_f32: needs no quieting of its operands, as fmaxf does)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
+}
 // largest / sum over the four groups of 16 lanes, and over the two halves of the wave
 __device__ __forceinline__ float max_halves(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(as_u32(x), as_u32(x), false, false);
-  return fmaxf(as_f32(r[0]), as_f32(r[1]));
+  return __builtin_elementwise_maximum(as_f32(r[0]), as_f32(r[1]));
 }
 __device__ __forceinline__ float sum_halves(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(as_u32(x), as_u32(x), false, false);
@@ -57,7 +61,7 @@ __device__ __forceinline__ float sum_halves(float x) {
 }
 __device__ __forceinline__ float max_groups(float x) {
   const auto r = __builtin_amdgcn_permlane16_swap(as_u32(x), as_u32(x), false, false);
-  return max_halves(fmaxf(as_f32(r[0]), as_f32(r[1])));
+  return max_halves(__builtin_elementwise_maximum(as_f32(r[0]), as_f32(r[1])));
 }
 __device__ __forceinline__ float sum_groups(float x) {
   const auto r = __builtin_amdgcn_permlane16_swap(as_u32(x), as_u32(x), false, false);
@@ -67,6 +71,9 @@ __device__ __forceinline__ float sum_groups(float x) {
 // a bf16 that is not finite: exponent bits all ones (either half of a word)
 __device__ __forceinline__ bool not_finite_bf16(uint32_t w) {
   return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u;
+}
+__device__ __forceinline__ uint32_t not_finite_halves(uint32_t w) {   // bit 0: the low half, bit 1: the high one
+  return ((w & 0x7F80u) == 0x7F80u ? 1u : 0u) | ((w & 0x7F800000u) == 0x7F800000u ? 2u : 0u);
 }
 // both halves: 0 where finite, 1.0 where not; and the word with such halves taken out
 __device__ __forceinline__ uint32_t marks_bf16(uint32_t w) {

@@ -10,6 +10,9 @@
 #pragma once
 #include "attend_common.hpp"
 
+#ifndef PV_AHEAD
+#define PV_AHEAD 3   // RING must divide STEPS
+#endif
 namespace tsdp {
 
 struct PromptArgs {
@@ -64,175 +67,324 @@ __device__ __forceinline__ void to_lds(const void* g, void* lds) {
 template <int CH> __device__ __forceinline__ int key_swizzle(int row) { return CH >= 16 ? row & 15 : CH == 8 ? (row >> 1) & 7 : (row >> 2) & 3; }
 template <int CH> __device__ __forceinline__ int value_swizzle(int row) { return CH >= 16 ? (row & 3) << 2 : CH == 8 ? ((row >> 1) & 1) << 2 : 0; }
 
+// The maximum m_i is that of the first 32 keys, and moves only where a score is 2^48 times its weight above it (each query by
+// its own scores): weights up to 2^48 lose nothing in floating types, and leave 2^59 to the values before a sum of 2^20 of
+// them overflows.
+constexpr float MOST_RISE = 48.f;
+constexpr int VM_NONE = 0x0F70;              // s_waitcnt vmcnt(0)
+
+// bf16.  A wave owns 32 queries.  Keys go by 32 (half a tile) through three stages that do not depend on each other and are
+// issued into each other: scores of the next 32 keys (matrix pipe), softmax of these (vector pipe), product of the last 32
+// with their values (matrix pipe).  Key tiles are two buffers, and so are value tiles, a tile behind: one barrier a tile, in
+// its middle, where the tiles requested at the last one have landed and the oldest buffers are free again.  Each buffer is a
+// variable of its own, so that the compiler sees that reads of one need not wait for loads into another.
+// Tiles that are masked for some query of the workgroup come last and go through the stages one by one -- and so does
+// everything, once more, where a maximum would have had to move on the way, which the overlapped loop only notices.
+// A weight of zero does not hide a value that is not finite from a matrix product.  Where some query does not see all of a
+// tile, such values are therefore zeroed in LDS by the wave that loaded them and noted in a bitmap (a byte for 8 dims), from which each
+// query that sees them collects the outputs that become NaN.
 template <int D, int NW>
 struct PromptBf16 {
-  static constexpr int KT = 64, CH = D / 8, TILE_B = KT * D * 2, ROUNDS = KT * CH / (NW * 64);
+  static constexpr int KT = 64, CH = D / 8, DT = D / 32, TILE_B = KT * D * 2, ROUNDS = KT * CH / (NW * 64);
   static constexpr int RPR = NW * 64 / CH;   // rows a round of loads
-  static_assert(ROUNDS >= 1 && KT * CH % (NW * 64) == 0, "a tile is whole rounds of the workgroup's loads");
+  static constexpr int TQ = 32 * NW;
+  static_assert(ROUNDS >= 1 && KT * CH % (NW * 64) == 0 && RPR % 16 == 0, "a tile is whole rounds of the workgroup's loads, swizzled alike");
 
-  static __device__ __forceinline__ bf16x8 read_key(const uint8_t* tile, int row, int chunk) {
+  f32x16 o[DT];
+  bf16x8 q[D / 16];
+  float m, l;
+
+  static __device__ __forceinline__ bf16x8 key(const uint8_t* tile, int row, int chunk) {
     return *reinterpret_cast<const bf16x8*>(tile + row * (D * 2) + ((chunk ^ key_swizzle<CH>(row)) << 4));
   }
-  // values of keys row .. row + 3 (row: of this lane's quarter) as a transposed operand of 4 keys: lane l gets dim l % 16
-  // of its group's 16 dims
-  static __device__ __forceinline__ u32x2 read_value(const uint8_t* tile, int row, int dim) {
-    const int chunk = dim >> 3;
-    const uint8_t* p = tile + row * (D * 2) + ((chunk ^ value_swizzle<CH>(row)) << 4) + (dim & 7) * 2;
+  // values of 8 keys as a transposed operand: lane l gets dim 32 d + l % 32 of keys 16 x + 4 h + {0..3, 8..11} of the 32 keys
+  // from row0 on (h = l / 32).  One read turns 4 keys x 16 dims for 16 lanes, each of which names 4 dims of one key.
+  static __device__ __forceinline__ u32x4 values(const uint8_t* tile, int row0, int x, int d, int lane) {
     typedef __attribute__((ext_vector_type(4))) short s16x4;
-    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p));
+    typedef __attribute__((address_space(3))) s16x4* at;
+    const int row = row0 + 16 * x + 4 * (lane >> 5) + ((lane & 15) >> 2), dim = 32 * d + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
+    const uint8_t* p = tile + row * (D * 2) + (((dim >> 3) ^ value_swizzle<CH>(row)) << 4) + (dim & 7) * 2;
+    const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)p));
+    const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)(p + 8 * (D * 2))));
+    return u32x4{lo[0], lo[1], hi[0], hi[1]};
+  }
+
+  __device__ __forceinline__ f32x16 scores(const uint8_t* kt, int row0, int lane) const {
+    f32x16 s = f32x16{};
+#pragma unroll
+    for (int x = 0; x < D / 16; ++x) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key(kt, row0 + (lane & 31), 2 * x + (lane >> 5)), q[x], s, 0, 0, 0);
+    return s;
+  }
+
+  // f: what sums and outputs so far have to be scaled by
+  __device__ __forceinline__ bool maximum(const f32x16& s, float c, float& f) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int x = 0; x < 16; x += 2) top = max3(top, s[x], s[x + 1]);
+    top = max_halves(top) * c;
+    const bool moves = top > m + MOST_RISE;
+    const float to = moves ? top : m;
+    f = moves ? __builtin_amdgcn_exp2f(m - to) : 1.f;
+    l *= f;
+    m = to;
+    return moves;
+  }
+  // weight of the key of register x
+  __device__ __forceinline__ void weight(const f32x16& s, float c, float sub, int x, bf16x8 (&p)[2]) {
+    const float e = __builtin_amdgcn_exp2f(fmaf(s[x], c, -sub));
+    l += e;
+    p[x / 8][x % 8] = (__bf16)e;             // rounded for the matrix cores: by at most 2^-8 of each weight
+  }
+  __device__ __forceinline__ float subtrahend() const { return m == -INFINITY ? 0.f : m; }
+
+  __device__ __forceinline__ void scale(float f) {
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) o[d][x] *= f;
+  }
+
+  __device__ __forceinline__ void product(const bf16x8 (&p)[2], const uint8_t* vt, int row0, int lane) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, values(vt, row0, x, d, lane)), p[x], o[d], 0, 0, 0);
+  }
+
+  // The three stages of 32 keys, step by step: `next` = scores of the keys at k_row of kt, weights of `s`, product of `last` with
+  // the values at v_row of vt; as many steps of the one product as of the other, in turns, their operands read AHEAD steps
+  // before -- those of the first steps by the call before (READY), where that is not on the other side of a barrier; MORE: the
+  // next call continues at rows + 32 of the same tiles.
+  static constexpr int KS = D / 16, STEPS = 2 * KS, AHEAD = PV_AHEAD < STEPS ? PV_AHEAD : STEPS - 1, RING = AHEAD + 1;
+  template <bool FIRST, bool LAST, bool READY, bool MORE>
+  __device__ __forceinline__ void half_tile(bf16x8 (&ring)[RING], f32x16& next, const f32x16& s, bf16x8 (&p)[2], const bf16x8 (&last)[2], float c,
+                                            const uint8_t* kt, int k_row, const uint8_t* vt, int v_row, int lane) {
+    static_assert(STEPS % RING == 0 || !(READY || MORE), "the ring goes on from one call to the next");
+    auto fetch = [&](int st) __attribute__((always_inline)) {
+      const int more = st >= STEPS ? 32 : 0, x = (st % STEPS) / 2;
+      if (more && !MORE) return;
+      if (st % 2 == 0) {
+        if (!LAST || more) ring[st % RING] = key(kt, k_row + more + (lane & 31), 2 * x + (lane >> 5));
+      } else {
+        if (!FIRST || more) ring[st % RING] = __builtin_bit_cast(bf16x8, values(vt, v_row + more, x / DT, x % DT, lane));
+      }
+    };
+    const float sub = subtrahend();
+    if (!READY) {
+#pragma unroll
+      for (int st = 0; st < AHEAD; ++st) fetch(st);
+    }
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) {
+      fetch(st + AHEAD);
+#pragma unroll
+      for (int x = st * 16 / STEPS; x < (st + 1) * 16 / STEPS; ++x) {
+        weight(s, c, sub, x, p);
+        asm volatile("" : "+v"(l));                                    // computed here, not where it is used
+        if (x % 8 == 7) asm volatile("" : "+v"(p[x / 8]));
+      }
+      const int i = st / 2;
+      if (st % 2 == 0) {
+        if constexpr (!LAST) next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[st % RING], q[i], i == 0 ? f32x16{} : next, 0, 0, 0);
+      } else {
+        if constexpr (!FIRST) o[i % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[st % RING], last[i / DT], o[i % DT], 0, 0, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
   }
 };
 
-template <int D, int NW>
-__global__ __launch_bounds__(NW * 64) void k_prompt_bf16(PromptArgs a) {
+template <int D, int NW, int WAVES>
+__global__ __launch_bounds__(NW * 64, WAVES) void k_prompt_bf16(PromptArgs a) {
   typedef PromptBf16<D, NW> C;
-  constexpr int KT = C::KT, CH = C::CH, DT = D / 32, TQ = 32 * NW;
-  __shared__ __align__(16) uint8_t lds[2][2][C::TILE_B];
+  constexpr int KT = C::KT, CH = C::CH;
+  __shared__ __align__(16) uint8_t k0[C::TILE_B], k1[C::TILE_B], v0[C::TILE_B], v1[C::TILE_B];   // tiles of even and odd number
   __shared__ uint32_t unusual[NW];           // some value of a masked tile is not finite, as each wave has seen it
+  __shared__ uint8_t where[2][KT * CH];      // which, a bit for each
+  __shared__ uint32_t rises[NW];             // some maximum would have had to move in the overlapped loop
   PromptTile t;
-  if (!prompt_tile<TQ>(a, t)) return;
+  if (!prompt_tile<C::TQ>(a, t)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5;
-  const int i0 = t.i0 + wave * 32, i = i0 + col;               // this lane's query
-  const int mine = i < t.nq ? seen(i, t.nq, t.nk, a.causal) : 0;
-  // keys that all / some queries of the wave see, and that some / all of the workgroup see
-  const int all = i0 >= t.nq ? 0 : seen(i0, t.nq, t.nk, a.causal);
-  const int some = i0 >= t.nq ? 0 : seen(min(i0 + 31, t.nq - 1), t.nq, t.nk, a.causal);
-  const int last = seen(min(t.i0 + TQ, t.nq) - 1, t.nq, t.nk, a.causal);
-  const int first = seen(t.i0, t.nq, t.nk, a.causal);
-  const int tiles = (last + KT - 1) / KT;
-  if (lane == 0) unusual[wave] = 0;
-
-  const __bf16* q = static_cast<const __bf16*>(a.q) + (int64_t)(t.q_lo + min(i, t.nq - 1)) * a.q_row + t.head * D;
-  bf16x8 qf[D / 16];
-#pragma unroll
-  for (int s = 0; s < D / 16; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(q + 16 * s + 8 * half);
+  const int i0 = t.i0 + wave * 32, i = i0 + col;               // the wave's first query, this lane's
+  // tiles that every query of the workgroup sees in full, and that some query sees
+  const int full = seen(t.i0, t.nq, t.nk, a.causal) / KT;
+  const int tiles = (seen(min(t.i0 + C::TQ, t.nq) - 1, t.nq, t.nk, a.causal) + KT - 1) / KT;
+  const int mine = i < t.nq ? seen(i, t.nq, t.nk, a.causal) : 0;                              // keys that this lane's query sees
+  const int some = i0 < t.nq ? seen(min(i0 + 31, t.nq - 1), t.nq, t.nk, a.causal) : 0;        // and that some query of the wave sees
+  if (lane == 0) { unusual[wave] = 0; rises[wave] = 0; }
 
   const __bf16* kb = static_cast<const __bf16*>(a.k) + (int64_t)t.k_lo * a.k_row + t.kv_head * D;
   const __bf16* vb = static_cast<const __bf16*>(a.v) + (int64_t)t.k_lo * a.v_row + t.kv_head * D;
   const int sr = wave * (64 / CH) + lane / CH, pc = lane % CH;
-  auto stage = [&](int tile, int buf) {
+  // this lane's bytes of the first round of a tile; rounds and tiles are whole rows further
+  const uint32_t k_off = (uint32_t)(sr * (int)a.k_row + (pc ^ key_swizzle<CH>(sr)) * 8) * 2;
+  const uint32_t v_off = (uint32_t)(sr * (int)a.v_row + (pc ^ value_swizzle<CH>(sr)) * 8) * 2;
+  auto stage = [&](const __bf16* base, int64_t row, uint32_t off, int tile, uint8_t* to) __attribute__((always_inline)) {
+    if (tile >= tiles) return;
+    const char* at = reinterpret_cast<const char*>(base + (int64_t)tile * KT * row);
+    const int left = t.nk - tile * KT;
+    if (left >= KT) {
 #pragma unroll
-    for (int n = 0; n < C::ROUNDS; ++n) {
-      const int r = n * C::RPR + sr;
-      const int64_t row = min(tile * KT + r, t.nk - 1);        // rows behind the sequence: its last one, masked
-      uint8_t* at = &lds[buf][0][0] + (n * NW + wave) * 1024;
-      to_lds(kb + row * a.k_row + (pc ^ key_swizzle<CH>(r)) * 8, at);
-      to_lds(vb + row * a.v_row + (pc ^ value_swizzle<CH>(r)) * 8, at + C::TILE_B);
+      for (int n = 0; n < C::ROUNDS; ++n) to_lds(at + (int64_t)n * C::RPR * row * 2 + off, to + (n * NW + wave) * 1024);
+    } else {                                 // rows behind the sequence: its last one, masked
+#pragma unroll 1
+      for (int n = 0; n < C::ROUNDS; ++n) {
+        const int over = max(n * C::RPR + sr - (left - 1), 0);
+        to_lds(at + ((int64_t)n * C::RPR - over) * row * 2 + off, to + (n * NW + wave) * 1024);
+      }
     }
   };
+#define TSDP_KEYS(N, TO) stage(kb, a.k_row, k_off, N, TO)
+#define TSDP_VALUES(N, TO) stage(vb, a.v_row, v_off, N, TO)
+  TSDP_KEYS(0, k0);
+  TSDP_KEYS(1, k1);
+  TSDP_VALUES(0, v0);
 
-  f32x16 o[DT];
+  C w;
+  const __bf16* q = static_cast<const __bf16*>(a.q) + (int64_t)(t.q_lo + min(i, t.nq - 1)) * a.q_row + t.head * D;
 #pragma unroll
-  for (int d = 0; d < DT; ++d) o[d] = f32x16{};
-  float m = -INFINITY, l = 0.f;
-  if (tiles > 0) stage(0, 0);
-  for (int n = 0; n < tiles; ++n) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    const uint8_t* kt = &lds[n & 1][0][0];
-    const uint8_t* vt = kt + C::TILE_B;
-    if ((n + 1) * KT > first) {              // masked for some wave: what this wave has loaded of the values is looked at
-      bool bad = false;
+  for (int x = 0; x < D / 16; ++x) w.q[x] = *reinterpret_cast<const bf16x8*>(q + 16 * x + 8 * half);
+  auto clear = [&]() __attribute__((always_inline)) {
+    w.m = -INFINITY; w.l = 0.f;
 #pragma unroll
-      for (int x = 0; x < C::ROUNDS; ++x) {
-        const u32x4 w = *reinterpret_cast<const u32x4*>(vt + (x * NW + wave) * 1024 + lane * 16);
-#pragma unroll
-        for (int y = 0; y < 4; ++y) bad |= not_finite_bf16(w[y]);
-      }
-      if (__ballot(bad) && lane == 0) unusual[wave] = 1;
+    for (int d = 0; d < C::DT; ++d) w.o[d] = f32x16{};
+  };
+  clear();
+
+  int from = 0;                              // first tile of the plain loop
+  if (full > 0) {
+    f32x16 s[2];
+    bf16x8 p[2][2], ring[C::RING];
+    float f;
+    __builtin_amdgcn_s_waitcnt(VM_NONE);
+    __syncthreads();
+    s[0] = w.scores(k0, 0, lane);
+    w.maximum(s[0], a.c, f);
+    // first and second half of a tile: K, V its buffers, KN the next tile's keys, VL the last one's values
+#define TSDP_FIRST(FIRST, K, VL) w.template half_tile<FIRST, false, !(FIRST), false>(ring, s[1], s[0], p[0], p[1], a.c, K, 32, VL, 32, lane)
+#define TSDP_SECOND(LAST, KN, V) w.template half_tile<false, LAST, false, !(LAST)>(ring, s[0], s[1], p[1], p[0], a.c, KN, 0, V, 0, lane)
+    // between them, in tile N with keys in K and the other buffer of values VN
+#define TSDP_MIDDLE(N, K, VN)                                                                                     \
+  do {                                                                                                            \
+    __builtin_amdgcn_s_waitcnt(VM_NONE);                                                                          \
+    __syncthreads();                                                                                              \
+    TSDP_KEYS((N) + 2, K);                                                                                        \
+    TSDP_VALUES((N) + 1, VN);                                                                                     \
+  } while (0)
+    TSDP_FIRST(true, k0, v1);
+    TSDP_MIDDLE(0, k0, v1);
+    int n = 0;
+    while (n + 1 < full) {
+      TSDP_SECOND(false, k1, v0);
+      TSDP_FIRST(false, k1, v0);
+      TSDP_MIDDLE(n + 1, k1, v0);
+      if (++n + 1 >= full) break;
+      TSDP_SECOND(false, k0, v1);
+      TSDP_FIRST(false, k0, v1);
+      TSDP_MIDDLE(n + 1, k0, v1);
+      ++n;
     }
-    __syncthreads();                         // the tile is there for all, and the other buffer read by all
-    if (n + 1 < tiles) stage(n + 1, (n + 1) & 1);
-    if (n * KT >= some) continue;
-    f32x16 s[2] = {f32x16{}, f32x16{}};
-#pragma unroll
-    for (int x = 0; x < D / 16; ++x)
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-        s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(C::read_key(kt, 32 * u + col, 2 * x + half), qf[x], s[u], 0, 0, 0);
-    const bool masked = (n + 1) * KT > all;
-    if (masked) {
-      const int left = mine - n * KT;        // keys of the tile that this query sees
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int x = 0; x < 16; ++x)
-          if (32 * u + 8 * (x / 4) + 4 * half + x % 4 >= left) s[u][x] = -INFINITY;
-    }
-    float top = s[0][0];
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int x = 0; x < 16; ++x) top = fmaxf(top, s[u][x]);
-    top = max_halves(top) * a.c;
-    // the running maximum moves only where it would grow by more than 2^8: powers stay below 2^8, and sums far from overflow
-    if (__any(top > m + 8.f)) {
-      const float to = top > m + 8.f ? top : m, f = to == m ? 1.f : __builtin_amdgcn_exp2f(m - to);   // each query by its own scores
-      m = to;
-      l *= f;
-#pragma unroll
-      for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int x = 0; x < 16; ++x) o[d][x] *= f;
-    }
-    const float sub = m == -INFINITY ? 0.f : m;
-    bf16x8 p[4];
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int x = 0; x < 16; ++x) {
-        const float e = __builtin_amdgcn_exp2f(fmaf(s[u][x], a.c, -sub));
-        l += e;
-        p[2 * u + x / 8][x % 8] = (__bf16)e;  // P rounded to bf16 for the matrix cores: at most 2^-8 of each weight
-      }
-    const int vrow = 4 * half + (lane & 15) / 4, vdim = ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
-    if (masked && any_of<NW>(unusual)) {
-      // values that are not finite are taken out of the product, and set the outputs of the queries that see them
-#pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        f32x16 marks = f32x16{};
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const u32x2 lo = C::read_value(vt, 16 * x + vrow, 32 * d + vdim), hi = C::read_value(vt, 16 * x + 8 + vrow, 32 * d + vdim);
-          const u32x4 w = {lo[0], lo[1], hi[0], hi[1]};
-          u32x4 fin, mark;
-#pragma unroll
-          for (int y = 0; y < 4; ++y) { fin[y] = finite_bf16(w[y]); mark[y] = marks_bf16(w[y]); }
-          bf16x8 sees;
-#pragma unroll
-          for (int y = 0; y < 8; ++y)
-            sees[y] = (__bf16)(n * KT + 16 * x + 8 * (y / 4) + 4 * half + y % 4 < mine ? 1.f : 0.f);
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fin), p[x], o[d], 0, 0, 0);
-          marks = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, mark), sees, marks, 0, 0, 0);
-        }
-#pragma unroll
-        for (int x = 0; x < 16; ++x)
-          if (marks[x] != 0.f) o[d][x] = NAN;
-      }
+    if (n & 1) {
+      TSDP_SECOND(true, k0, v1);
+      w.product(p[1], v1, 32, lane);
     } else {
-#pragma unroll
-      for (int x = 0; x < 4; ++x)
-#pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          const u32x2 lo = C::read_value(vt, 16 * x + vrow, 32 * d + vdim), hi = C::read_value(vt, 16 * x + 8 + vrow, 32 * d + vdim);
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]}), p[x], o[d], 0, 0, 0);
-        }
+      TSDP_SECOND(true, k1, v0);
+      w.product(p[1], v0, 32, lane);
+    }
+#undef TSDP_FIRST
+#undef TSDP_SECOND
+#undef TSDP_MIDDLE
+    if (__any(w.l > __builtin_amdgcn_exp2f(MOST_RISE)) && lane == 0) rises[wave] = 1;   // some weight was more, or infinite
+    __syncthreads();
+    from = full;
+    if (any_of<NW>(rises)) {                 // once more from the start
+      from = 0;
+      __builtin_amdgcn_s_waitcnt(VM_NONE);
+      __syncthreads();                       // nobody's loads land behind the new ones
+      TSDP_KEYS(0, k0);
+      TSDP_KEYS(1, k1);
+      TSDP_VALUES(0, v0);
+      clear();
     }
   }
-  l = sum_halves(l);
-  if (i >= t.nq) return;
-  const float r = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;      // no key seen: zeros; NaN stays
-  __bf16* out = static_cast<__bf16*>(a.out) + (int64_t)(t.q_lo + i) * a.out_row + t.head * D;
+  uint32_t gone[C::DT];                      // outputs that a visible value makes NaN: bit 8 j + e of word d is o[d][4 j + e]
 #pragma unroll
-  for (int d = 0; d < DT; ++d)
+  for (int d = 0; d < C::DT; ++d) gone[d] = 0;
+  auto plain = [&](int n, uint8_t* k, uint8_t* kn, uint8_t* v, uint8_t* vn) __attribute__((always_inline)) {
+    __builtin_amdgcn_s_waitcnt(VM_NONE);
+    bool bad = false;
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      bf16x4 y;
+    for (int x = 0; x < C::ROUNDS; ++x) {
+      u32x4* at = reinterpret_cast<u32x4*>(v + (x * NW + wave) * 1024 + lane * 16);
+      u32x4 y = *at;
+      uint32_t marks = 0;
 #pragma unroll
-      for (int z = 0; z < 4; ++z) y[z] = (__bf16)(o[d][4 * x + z] * r);
-      *reinterpret_cast<bf16x4*>(out + 32 * d + 8 * x + 4 * half) = y;
+      for (int z = 0; z < 4; ++z) marks |= not_finite_halves(y[z]) << (2 * z);
+      where[n & 1][(x * C::RPR + sr) * CH + (pc ^ value_swizzle<CH>(sr))] = (uint8_t)marks;
+      if (marks) {
+        bad = true;
+#pragma unroll
+        for (int z = 0; z < 4; ++z) y[z] = finite_bf16(y[z]);
+        *at = y;
+      }
     }
-  if (a.lse && half == 0) a.lse[(int64_t)(t.q_lo + i) * a.heads + t.head] = (m + __builtin_amdgcn_logf(l)) * LN2;
+    if (__any(bad) && lane == 0) unusual[wave] = 1;
+    __syncthreads();
+    if (n > from) TSDP_KEYS(n + 1, kn);
+    TSDP_VALUES(n + 1, vn);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int left = mine - (n * KT + 32 * u);
+      if (n * KT + 32 * u >= some) continue;
+      f32x16 s = w.scores(k, 32 * u, lane);
+      bf16x8 p[2];
+#pragma unroll
+      for (int x = 0; x < 16; ++x)
+        if (8 * (x / 4) + 4 * half + x % 4 >= left) s[x] = -INFINITY;
+      float f;
+      if (__any(w.maximum(s, a.c, f))) w.scale(f);
+      const float sub = w.subtrahend();
+#pragma unroll
+      for (int x = 0; x < 16; ++x) w.weight(s, a.c, sub, x, p);
+      w.product(p, v, 32 * u, lane);
+    }
+    if (any_of<NW>(unusual)) {
+      const int left = min(mine - n * KT, KT);
+#pragma unroll 1
+      for (int j = 0; j < left; ++j)
+#pragma unroll
+        for (int d = 0; d < C::DT; ++d) gone[d] |= *reinterpret_cast<const uint32_t*>(&where[n & 1][j * CH + 4 * d]) >> (4 * half) & 0x0F0F0F0Fu;
+    }
+  };
+  for (int n = from; n < tiles; ++n) {
+    if (n & 1) plain(n, k1, k0, v1, v0);
+    else plain(n, k0, k1, v0, v1);
+  }
+#undef TSDP_KEYS
+#undef TSDP_VALUES
+  const float l = sum_halves(w.l);
+  const float r = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;      // no key seen: zeros; NaN stays
+  __bf16* out = static_cast<__bf16*>(a.out) + (int64_t)(t.q_lo + i) * a.out_row + t.head * D + 8 * half;
+#pragma unroll
+  for (int d = 0; d < C::DT; ++d)
+#pragma unroll
+    for (int x = 0; x < 4; x += 2) {         // the halves of the wave hold dims 0..3 and 4..7 of each eight: one takes all of the first
+      u32x2 y[2];                            // eight, the other of the second
+#pragma unroll
+      for (int z = 0; z < 2; ++z)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int at = 4 * (x + z) + 2 * e, bit = 8 * (x + z) + 2 * e;
+          const float lo = gone[d] >> bit & 1 ? NAN : w.o[d][at] * r, hi = gone[d] >> (bit + 1) & 1 ? NAN : w.o[d][at + 1] * r;
+          y[z][e] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)lo, (__bf16)hi});
+        }
+      const auto s0 = __builtin_amdgcn_permlane32_swap(y[0][0], y[1][0], false, false);
+      const auto s1 = __builtin_amdgcn_permlane32_swap(y[0][1], y[1][1], false, false);
+      if (i < t.nq) *reinterpret_cast<u32x4*>(out + 32 * d + 8 * x) = u32x4{s0[0], s1[0], s0[1], s1[1]};
+    }
+  if (a.lse && half == 0 && i < t.nq) a.lse[(int64_t)(t.q_lo + i) * a.heads + t.head] = (w.m + __builtin_amdgcn_logf(l)) * LN2;
 }
 
 // fp32: the same walk with mfma_f32_32x32x2_f32.  A lane's 16-byte chunk of a key feeds four of them (MFMA j contracts dims
