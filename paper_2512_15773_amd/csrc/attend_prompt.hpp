@@ -10,9 +10,7 @@
 #pragma once
 #include "attend_common.hpp"
 
-#ifndef PV_AHEAD
-#define PV_AHEAD 3   // RING must divide STEPS
-#endif
+
 namespace tsdp {
 
 struct PromptArgs {
@@ -156,7 +154,7 @@ struct PromptBf16 {
   // the values at v_row of vt; as many steps of the one product as of the other, in turns, their operands read AHEAD steps
   // before -- those of the first steps by the call before (READY), where that is not on the other side of a barrier; MORE: the
   // next call continues at rows + 32 of the same tiles.
-  static constexpr int KS = D / 16, STEPS = 2 * KS, AHEAD = PV_AHEAD < STEPS ? PV_AHEAD : STEPS - 1, RING = AHEAD + 1;
+  static constexpr int KS = D / 16, STEPS = 2 * KS, AHEAD = 3, RING = AHEAD + 1;
   template <bool FIRST, bool LAST, bool READY, bool MORE>
   __device__ __forceinline__ void half_tile(bf16x8 (&ring)[RING], f32x16& next, const f32x16& s, bf16x8 (&p)[2], const bf16x8 (&last)[2], float c,
                                             const uint8_t* kt, int k_row, const uint8_t* vt, int v_row, int lane) {
@@ -195,7 +193,9 @@ struct PromptBf16 {
   }
 };
 
-template <int D, int NW, int WAVES>
+// OVERLAP: with the overlapped loop, 2 waves a SIMD; without it (the same results, bit for bit) there is room for more waves to
+// hide each other's loads, which pays where sequences are short.
+template <int D, int NW, int WAVES, bool OVERLAP>
 __global__ __launch_bounds__(NW * 64, WAVES) void k_prompt_bf16(PromptArgs a) {
   typedef PromptBf16<D, NW> C;
   constexpr int KT = C::KT, CH = C::CH;
@@ -209,7 +209,7 @@ __global__ __launch_bounds__(NW * 64, WAVES) void k_prompt_bf16(PromptArgs a) {
   const int col = lane & 31, half = lane >> 5;
   const int i0 = t.i0 + wave * 32, i = i0 + col;               // the wave's first query, this lane's
   // tiles that every query of the workgroup sees in full, and that some query sees
-  const int full = seen(t.i0, t.nq, t.nk, a.causal) / KT;
+  const int full = OVERLAP ? seen(t.i0, t.nq, t.nk, a.causal) / KT : 0;
   const int tiles = (seen(min(t.i0 + C::TQ, t.nq) - 1, t.nq, t.nk, a.causal) + KT - 1) / KT;
   const int mine = i < t.nq ? seen(i, t.nq, t.nk, a.causal) : 0;                              // keys that this lane's query sees
   const int some = i0 < t.nq ? seen(min(i0 + 31, t.nq - 1), t.nq, t.nk, a.causal) : 0;        // and that some query of the wave sees
@@ -254,7 +254,7 @@ __global__ __launch_bounds__(NW * 64, WAVES) void k_prompt_bf16(PromptArgs a) {
   clear();
 
   int from = 0;                              // first tile of the plain loop
-  if (full > 0) {
+  if constexpr (OVERLAP) if (full > 0) {
     f32x16 s[2];
     bf16x8 p[2][2], ring[C::RING];
     float f;
