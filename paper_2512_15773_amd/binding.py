@@ -109,8 +109,8 @@ def _ptr(t, dtype=None):
 
 
 def _stream(stream):
-    s = torch.cuda.current_stream() if stream is None else stream
-    return s.cuda_stream
+    # the handle alone: building torch's Stream object takes 3 us
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) if stream is None else stream.cuda_stream
 
 
 _TYPE = {torch.float32: 0, torch.bfloat16: 1}
@@ -118,14 +118,19 @@ _TYPE = {torch.float32: 0, torch.bfloat16: 1}
 
 def _rows(t, heads, dim, dtype, dev):
     """Pointer and row stride of packed rows [rows, heads, dim]; the rows may be slices of wider ones."""
+    assert t.dtype is dtype and t.dim() == 3, f"expected [rows, {heads}, {dim}] of {dtype}, got {tuple(t.shape)} of {t.dtype}"
+    rows, h, d = t.shape
+    row, head, one = t.stride()
+    assert h == heads and d == dim, f"expected [rows, {heads}, {dim}], got {tuple(t.shape)}"
     assert t.get_device() == dev, "packed rows must be on the current device"
-    assert t.dtype == dtype, f"expected {dtype}, got {t.dtype}"
-    assert t.dim() == 3 and t.shape[1:] == (heads, dim), f"expected [rows, {heads}, {dim}], got {tuple(t.shape)}"
-    rows, row = t.shape[0], t.stride(0)
-    if rows <= 1 or t.numel() == 0:
-        row = heads * dim
-    assert t.stride(2) == 1 and (heads == 1 or t.stride(1) == dim), "the heads of a row must be next to each other"
-    return t.data_ptr(), row
+    assert one == 1 and (head == dim or heads == 1), "the heads of a row must be next to each other"
+    return t.data_ptr(), row if rows > 1 else heads * dim
+
+
+def _table(t, n, dev):
+    """Pointer of an int32 device tensor of n entries."""
+    assert t.dtype is torch.int32 and t.get_device() == dev and t.is_contiguous() and t.numel() == n, f"expected {n} contiguous int32 on the current device"
+    return t.data_ptr()
 
 
 class KvCache:
@@ -147,6 +152,7 @@ class KvCache:
         self.c = TsdpKvCache(type=held[k.dtype], kv_heads=kv, head_dim=dim, page_tokens=page, pages=pages, B=page_table.shape[0],
                              columns=page_table.shape[1], d_k=_ptr(k), d_v=_ptr(v), d_k_scale=_ptr(k_scale, torch.uint8),
                              d_v_scale=_ptr(v_scale, torch.uint8), d_page_table=_ptr(page_table, torch.int32))
+        self.ref = C.byref(self.c)
 
     @classmethod
     def alloc(cls, dtype, pages, kv_heads, page_tokens, head_dim, page_table):
@@ -347,13 +353,14 @@ class Tsdp:
 
     def _cache_rows(self, call, cache, row_ptr, start, k, v, stream):
         dev = torch.cuda.current_device()
+        dtype, rows, B = k.dtype, k.shape[0], start.shape[0]
         assert cache.device == dev, "the cache must be on the current device"
-        kp, k_row = _rows(k, cache.kv_heads, cache.head_dim, k.dtype, dev)
-        vp, v_row = _rows(v, cache.kv_heads, cache.head_dim, k.dtype, dev)
-        assert k.dtype in _TYPE and k.shape[0] == v.shape[0], "rows of keys and values must be alike, float32 or bfloat16"
-        assert row_ptr.shape[0] == start.shape[0] + 1, "row_ptr has one entry more than start"
-        self._chk(call(self.ctx, cache.c, start.shape[0], k.shape[0], _TYPE[k.dtype], _ptr(row_ptr, torch.int32), _ptr(start, torch.int32),
-                       kp, k_row, vp, v_row, _stream(stream)))
+        assert dtype in _TYPE and v.shape[0] == rows, "rows of keys and values must be alike, float32 or bfloat16"
+        kp, k_row = _rows(k, cache.kv_heads, cache.head_dim, dtype, dev)
+        vp, v_row = _rows(v, cache.kv_heads, cache.head_dim, dtype, dev)
+        rc = call(self.ctx, cache.ref, B, rows, _TYPE[dtype], _table(row_ptr, B + 1, dev), _table(start, B, dev), kp, k_row, vp, v_row, _stream(stream))
+        if rc:
+            self._chk(rc)
 
     def tsdp_cache_write(self, cache, row_ptr, start, k, v, stream=None):
         """Rows row_ptr[b] .. of k, v [rows, kv_heads, head_dim] to positions start[b] .. of environment b."""
@@ -362,32 +369,38 @@ class Tsdp:
     def tsdp_cache_read(self, cache, row_ptr, start, rows, dtype, out=None, stream=None):
         """Positions start[b] .. of every environment as packed rows (k, v); out: such a pair to write into."""
         if out is None:
-            out = tuple(torch.empty(rows, cache.kv_heads, cache.head_dim, dtype=dtype, device=row_ptr.device) for _ in "kv")
-        assert out[0].dtype == dtype and out[0].shape[0] == rows, "out must hold `rows` rows of the given type"
+            both = torch.empty((2, rows, cache.kv_heads, cache.head_dim), dtype=dtype, device=row_ptr.device)
+            out = both[0], both[1]
+        assert out[0].dtype is dtype and out[0].shape[0] == rows, "out must hold `rows` rows of the given type"
         self._cache_rows(self.lib.tsdp_cache_read, cache, row_ptr, start, out[0], out[1], stream)
         return out
 
     @staticmethod
     def _lse(lse, rows, heads, dev):
-        assert lse is None or (tuple(lse.shape) == (rows, heads) and lse.get_device() == dev), f"lse must be [{rows}, {heads}]"
+        if lse is None:
+            return None
+        assert tuple(lse.shape) == (rows, heads) and lse.get_device() == dev, f"lse must be [{rows}, {heads}]"
         return _ptr(lse, torch.float32)
 
     def tsdp_attend_prompt(self, q, k, v, q_ptr, k_ptr=None, *, causal=True, scale=None, out=None, lse=None, stream=None):
         """q [rows, q_heads, head_dim] (float32 or bfloat16), k, v [rows of keys, kv_heads, head_dim]; returns out."""
         dev = torch.cuda.current_device()
-        heads, dim, kv = q.shape[1], q.shape[2], k.shape[1]
+        dtype = q.dtype
+        (rows, heads, dim), (k_rows, kv, _) = q.shape, k.shape
+        assert dtype in _TYPE and v.shape[0] == k_rows, "q, k and v must be of one type, float32 or bfloat16, and k and v alike"
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        qp, q_row = _rows(q, heads, dim, q.dtype, dev)
-        kp, k_row = _rows(k, kv, dim, q.dtype, dev)
-        vp, v_row = _rows(v, kv, dim, q.dtype, dev)
-        op, out_row = _rows(out, heads, dim, q.dtype, dev)
-        assert q.dtype in _TYPE and out.shape == q.shape and v.shape[0] == k.shape[0], "q and out, k and v must be alike, float32 or bfloat16"
-        assert k_ptr is None or k_ptr.shape == q_ptr.shape, "q_ptr and k_ptr must be of one length"
-        h = TsdpHeads(_TYPE[q.dtype], heads, kv, dim, 1 if causal else 0, dim ** -0.5 if scale is None else scale)
-        self._chk(self.lib.tsdp_attend_prompt(self.ctx, h, q_ptr.shape[0] - 1, q.shape[0], k.shape[0], _ptr(q_ptr, torch.int32),
-                                              _ptr(k_ptr, torch.int32), qp, q_row, kp, k_row, vp, v_row, op, out_row,
-                                              self._lse(lse, q.shape[0], heads, dev), _stream(stream)))
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        assert out.shape[0] == rows, "out must be alike q"
+        qp, q_row = _rows(q, heads, dim, dtype, dev)
+        kp, k_row = _rows(k, kv, dim, dtype, dev)
+        vp, v_row = _rows(v, kv, dim, dtype, dev)
+        op, out_row = _rows(out, heads, dim, dtype, dev)
+        n = q_ptr.shape[0]
+        rc = self.lib.tsdp_attend_prompt(self.ctx, TsdpHeads(_TYPE[dtype], heads, kv, dim, 1 if causal else 0, dim ** -0.5 if scale is None else scale),
+                                         n - 1, rows, k_rows, _table(q_ptr, n, dev), None if k_ptr is None else _table(k_ptr, n, dev),
+                                         qp, q_row, kp, k_row, vp, v_row, op, out_row, self._lse(lse, rows, heads, dev), _stream(stream))
+        if rc:
+            self._chk(rc)
         return out
 
     def alloc_scratch(self, cache, q_heads, tokens, max_len, B=None):
@@ -403,23 +416,25 @@ class Tsdp:
         """q [B * tokens, q_heads, head_dim] over the first length[b] tokens of the cache; returns out (out_dtype: float32 or
         that of q).  scratch: from alloc_scratch (allocated for the call where it is left out)."""
         dev = torch.cuda.current_device()
-        assert cache.device == dev and length.get_device() == dev, "cache and lengths must be on the current device"
+        dtype, B = q.dtype, length.shape[0]
         rows, heads, dim = q.shape
-        B = length.shape[0]
-        assert q.dtype in _TYPE and rows == B * tokens and dim == cache.head_dim, "q must be [B * tokens, q_heads, head_dim], float32 or bfloat16"
+        assert cache.device == dev, "the cache must be on the current device"
+        assert dtype in _TYPE and rows == B * tokens and dim == cache.head_dim, "q must be [B * tokens, q_heads, head_dim], float32 or bfloat16"
         if out is None:
-            out = torch.empty(q.shape, dtype=out_dtype or q.dtype, device=q.device)
-        assert out.dtype in _TYPE and out.shape == q.shape and out_dtype in (None, out.dtype), "out must be alike q, float32 or bfloat16"
+            out = torch.empty_like(q, dtype=out_dtype, memory_format=torch.contiguous_format)
+        assert out.dtype in _TYPE and out.shape[0] == rows and out_dtype in (None, out.dtype), "out must be alike q, float32 or bfloat16"
         if scratch is None:
             scratch = self.alloc_scratch(cache, heads, tokens, max_len, B)
             if scratch is not None and stream is not None:
                 scratch.record_stream(stream)
-        qp, q_row = _rows(q, heads, dim, q.dtype, dev)
+        qp, q_row = _rows(q, heads, dim, dtype, dev)
         op, out_row = _rows(out, heads, dim, out.dtype, dev)
-        h = TsdpHeads(_TYPE[q.dtype], heads, cache.kv_heads, dim, 1 if causal else 0, dim ** -0.5 if scale is None else scale)
-        self._chk(self.lib.tsdp_attend_paged(self.ctx, h, cache.c, B, tokens, max_len, _ptr(length, torch.int32), qp, q_row,
-                                             _TYPE[out.dtype], op, out_row, self._lse(lse, rows, heads, dev), _ptr(scratch),
-                                             0 if scratch is None else scratch.numel() * scratch.element_size(), _stream(stream)))
+        rc = self.lib.tsdp_attend_paged(self.ctx, TsdpHeads(_TYPE[dtype], heads, cache.kv_heads, dim, 1 if causal else 0, dim ** -0.5 if scale is None else scale),
+                                        cache.ref, B, tokens, max_len, _table(length, B, dev), qp, q_row, _TYPE[out.dtype], op, out_row,
+                                        self._lse(lse, rows, heads, dev), _ptr(scratch),
+                                        0 if scratch is None else scratch.numel() * scratch.element_size(), _stream(stream))
+        if rc:
+            self._chk(rc)
         return out
 
     def tsdp_kernel_timing(self, enable):
