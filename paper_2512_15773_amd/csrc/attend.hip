@@ -92,10 +92,16 @@ void launch_prompt(int type, PromptArgs a, hipStream_t s) {
   hipLaunchKernelGGL((k_prompt_bf16<D, 4, 2, true>), grid, dim3(256), 0, s, a);
 }
 
+template <int D, int HELD, bool QF32, int NP, int NC, typename Out>
+void launch_paged_tiles(const PagedArgs& a, hipStream_t s) {
+  const int ct = (a.cols + 16 * NC - 1) / (16 * NC);
+  hipLaunchKernelGGL((k_paged<D, HELD, QF32, NP, NC, Out>), dim3((unsigned)((int64_t)a.B * ct * a.cache.kv_heads), a.max_chunks), dim3(256), 0, s, a);
+}
 template <int D, int HELD, bool QF32, int NP, typename Out>
 void launch_paged(const PagedArgs& a, hipStream_t s) {
-  const int ct = (a.cols + 15) / 16;
-  hipLaunchKernelGGL((k_paged<D, HELD, QF32, NP, Out>), dim3((unsigned)((int64_t)a.B * ct * a.cache.kv_heads), a.max_chunks), dim3(256), 0, s, a);
+  constexpr int MOST = HELD == HELD_F32 || QF32 ? 1 : D == 128 ? 2 : 4;
+  if (MOST > 1 && a.cols > 16) launch_paged_tiles<D, HELD, QF32, NP, MOST, Out>(a, s);
+  else launch_paged_tiles<D, HELD, QF32, NP, 1, Out>(a, s);
   if (a.max_chunks > 1)
     hipLaunchKernelGGL((k_paged_join<D, Out>), dim3((unsigned)((int64_t)a.B * a.cache.kv_heads * a.cols)), dim3(256), 0, s, a);
 }

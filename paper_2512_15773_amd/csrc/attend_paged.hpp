@@ -39,6 +39,15 @@ __device__ __forceinline__ int paged_len(const PagedArgs& a, int b) {
 
 template <int D, int HELD> struct PagedTile;
 
+// AHEAD: registers hold two tiles; WAVES: waves a SIMD that they leave room for
+#ifndef PWV
+#define PWV 2
+#endif
+template <int D, int HELD, int NC> struct PagedShape {
+  static constexpr bool AHEAD = !(HELD == HELD_F32 && D == 128);
+  static constexpr int WAVES = PWV;
+};
+
 template <int D> struct PagedTile<D, HELD_BF16> {
   u32x4 k[2][D / 32];
   uint32_t v[8][D / 32];
@@ -144,76 +153,58 @@ __device__ __forceinline__ void split(float x, __bf16 (&p)[NP]) {
   }
 }
 
+// One wave's share: NC tiles of 16 columns, a running softmax for each.
 // QF32: queries are fp32.  NP: bf16 parts of P (unused where the cache is fp32).
-template <int D, int HELD, bool QF32, int NP, typename Out>
-__global__ __launch_bounds__(256) void k_paged(PagedArgs a) {
-  constexpr bool F32 = HELD == HELD_F32;
-  constexpr int NQ = QF32 && !F32 ? 3 : 1, F = D / 16, OP = D + 4;
-  __shared__ __align__(16) float o_lds[4][16][OP];
-  __shared__ float ml_lds[4][16][2];
-  const int kv = a.cache.kv_heads, ct = (a.cols + 15) / 16;
-  const int kvh = blockIdx.x % kv, rest = blockIdx.x / kv, col0 = (rest % ct) * 16, b = rest / ct, chunk = blockIdx.y;
-  const int len = paged_len(a, b);
-  const int shift = chunk_shift(len, a.cols), chunks = chunks_of(len, a.cols);
-  if (chunk > 0 && chunk >= chunks) return;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
-  const int G = a.heads / kv, col = col0 + r, at = min(col, a.cols - 1);
-  const int token = at / G, head = kvh * G + at % G;
-  const int mine = col < a.cols ? seen(token, a.tokens, len, a.causal) : 0;
-  const int all = seen(col0 / G, a.tokens, len, a.causal);       // keys that every column of the tile sees
+template <int D, int HELD, bool QF32, int NP, int NC>
+struct PagedWave {
+  static constexpr bool F32 = HELD == HELD_F32;
+  static constexpr int NQ = QF32 && !F32 ? 3 : 1, F = D / 16;
+  typedef PagedTile<D, HELD> Tile;
+  bf16x8 q[NC][F32 ? 1 : NQ][F32 ? 1 : D / 32];
+  f32x4 qx[NC][F32 ? F : 1];
+  f32x4 o[NC][F];
+  float m[NC], l[NC];
+  int mine[NC];                              // keys that this lane's column sees
+  uint32_t gone[NC];                         // outputs that a visible value makes NaN
 
-  const int64_t q_at = ((int64_t)b * a.tokens + token) * a.q_row + head * D;
-  bf16x8 qf[NQ][D / 32];
-  f32x4 qx[F];
-  if constexpr (F32) {
+  __device__ __forceinline__ void start(int n, const void* at, int64_t off, int g) {
+    if constexpr (F32) {
 #pragma unroll
-    for (int x = 0; x < F; ++x) qx[x] = *reinterpret_cast<const f32x4*>(static_cast<const float*>(a.q) + q_at + 16 * x + 4 * g);
-  } else {
+      for (int x = 0; x < F; ++x) qx[n][x] = *reinterpret_cast<const f32x4*>(static_cast<const float*>(at) + off + 16 * x + 4 * g);
+    } else {
 #pragma unroll
-    for (int x = 0; x < D / 32; ++x) {
-      const int d = PagedTile<D, HELD>::q_dim(x, g);
-      if constexpr (QF32) {
-        const float* p = static_cast<const float*>(a.q) + q_at + d;
+      for (int x = 0; x < D / 32; ++x) {
+        const int d = Tile::q_dim(x, g);
+        if constexpr (QF32) {
+          const float* p = static_cast<const float*>(at) + off + d;
 #pragma unroll
-        for (int y = 0; y < 8; ++y) {
-          __bf16 parts[3];
-          split<3>(p[y], parts);
+          for (int y = 0; y < 8; ++y) {
+            __bf16 parts[3];
+            split<3>(p[y], parts);
 #pragma unroll
-          for (int z = 0; z < 3; ++z) qf[z][x][y] = parts[z];
+            for (int z = 0; z < 3; ++z) q[n][z][x][y] = parts[z];
+          }
+        } else {
+          q[n][0][x] = *reinterpret_cast<const bf16x8*>(static_cast<const __bf16*>(at) + off + d);
         }
-      } else {
-        qf[0][x] = *reinterpret_cast<const bf16x8*>(static_cast<const __bf16*>(a.q) + q_at + d);
       }
     }
   }
+  __device__ __forceinline__ void clear(int n) {
+#pragma unroll
+    for (int f = 0; f < F; ++f) o[n][f] = f32x4{};
+    m[n] = -INFINITY; l[n] = 0.f; gone[n] = 0;
+  }
 
-  f32x4 o[F];
-#pragma unroll
-  for (int f = 0; f < F; ++f) o[f] = f32x4{};
-  float m = -INFINITY, l = 0.f;
-  const int per_wave = 1 << (shift - 2);                         // keys of a wave
-  const long lo = ((long)chunk << shift) + wave * per_wave, hi = min(lo + per_wave, (long)len);
-  for (long k0 = lo; k0 < hi; k0 += 32) {
-    int64_t row[2];
-    bool ok[2];
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {                                // 16 keys lie in one page
-      const long pos = k0 + 16 * s;
-      const int page = pos < len ? page_of(a.cache, b, pos >> a.cache.page_shift) : 0;
-      ok[s] = page >= 0;
-      if (!ok[s] && lane == 0) report(a.status, STATUS_PAGE);
-      row[s] = pool_row(a.cache, max(page, 0), kvh, (int)(pos & ((1L << a.cache.page_shift) - 1)));
-    }
-    PagedTile<D, HELD> t;
-    t.load(a.cache, row, lane);
-    f32x4 s[2] = {f32x4{}, f32x4{}};
+  __device__ __forceinline__ void scores(const Tile& t, int n, f32x4 (&s)[2], int lane) const {
+    s[0] = f32x4{}; s[1] = f32x4{};
     if constexpr (F32) {
 #pragma unroll
       for (int x = 0; x < F; ++x)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
-          for (int u = 0; u < 2; ++u) s[u] = __builtin_amdgcn_mfma_f32_16x16x4f32(t.k[u][x][j], qx[x][j], s[u], 0, 0, 0);
+          for (int u = 0; u < 2; ++u) s[u] = __builtin_amdgcn_mfma_f32_16x16x4f32(t.k[u][x][j], qx[n][x][j], s[u], 0, 0, 0);
     } else {
 #pragma unroll
       for (int x = 0; x < D / 32; ++x)
@@ -221,148 +212,295 @@ __global__ __launch_bounds__(256) void k_paged(PagedArgs a) {
         for (int u = 0; u < 2; ++u) {
           const bf16x8 key = t.key(u, x, lane);
 #pragma unroll
-          for (int z = NQ - 1; z >= 0; --z) s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, qf[z][x], s[u], 0, 0, 0);
+          for (int z = NQ - 1; z >= 0; --z) s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q[n][z][x], s[u], 0, 0, 0);
         }
     }
-    const bool masked = k0 + 32 > all || !ok[0] || !ok[1];
-    bool sees[8];
-    if (masked) {
+  }
+  static __device__ __forceinline__ float largest(const f32x4 (&s)[2]) {
+    const float top = max3(max3(s[0][0], s[0][1], s[0][2]), s[0][3], s[1][0]);
+    return max_groups(max3(max3(top, s[1][1], s[1][2]), s[1][3], s[1][3]));
+  }
+  __device__ __forceinline__ void weights(const f32x4 (&s)[2], int n, float c, float (&p)[8]) {
+    const float sub = m[n] == -INFINITY ? 0.f : m[n];
 #pragma unroll
-      for (int x = 0; x < 8; ++x) {
-        sees[x] = ok[x / 4] && k0 + 16 * (x / 4) + 4 * g + x % 4 < mine;
-        if (!sees[x]) s[x / 4][x % 4] = -INFINITY;
-      }
+    for (int x = 0; x < 8; ++x) {
+      p[x] = __builtin_amdgcn_exp2f(fmaf(s[x / 4][x % 4], c, -sub));
+      l[n] += p[x];
     }
-    float top = s[0][0];
+  }
+
+  // 32 keys that every column sees.  FIRST: their maximum is taken; afterwards it stays, and a rise above it shows in the sums.
+  template <bool FIRST>
+  __device__ __forceinline__ void step(const Tile& t, float c, int lane) {
+    float p[NC][8];
 #pragma unroll
-    for (int x = 1; x < 8; ++x) top = fmaxf(top, s[x / 4][x % 4]);
-    top = max_groups(top) * a.c;
-    // the running maximum moves only where it would grow by more than 2^8
-    if (__any(top > m + 8.f)) {
-      const float to = top > m + 8.f ? top : m, f = to == m ? 1.f : __builtin_amdgcn_exp2f(m - to);   // each query by its own scores
-      m = to;
-      l *= f;
+    for (int n = 0; n < NC; ++n) {
+      f32x4 s[2];
+      scores(t, n, s, lane);
+      if (FIRST) {
+        const float top = largest(s) * c;
+        m[n] = top > -INFINITY ? top : -INFINITY;
+      }
+      weights(s, n, c, p[n]);
+    }
+    if constexpr (F32) {
+      product_f32(t.v, p);
+    } else {
+      uint32_t w[8][D / 32];
+      t.values(w, lane);
+      product_bf16(w, p);
+    }
+  }
+  __device__ __forceinline__ bool rose() const {
+    bool r = false;
+#pragma unroll
+    for (int n = 0; n < NC; ++n) r |= l[n] > most_sum(m[n]);
+    return __any(r);
+  }
+
+  // Any 32 keys from position k0 on.  ok: their halves' pages are inside the pool.
+  __device__ __forceinline__ void masked_step(Tile& t, long k0, bool ok0, bool ok1, float c, int lane) {
+    const int g = lane >> 4;
+    float p[NC][8];
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+      f32x4 s[2];
+      scores(t, n, s, lane);
+#pragma unroll
+      for (int x = 0; x < 8; ++x)
+        if (!sees(n, x, k0, ok0, ok1, g)) s[x / 4][x % 4] = -INFINITY;
+      const float top = largest(s) * c, to = top > m[n] + MOST_RISE ? top : m[n], f = to == m[n] ? 1.f : __builtin_amdgcn_exp2f(m[n] - to);
+      m[n] = to;
+      l[n] *= f;
 #pragma unroll
       for (int y = 0; y < F; ++y)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) o[y][x] *= f;
+        for (int x = 0; x < 4; ++x) o[n][y][x] *= f;
+      weights(s, n, c, p[n]);
     }
-    const float sub = m == -INFINITY ? 0.f : m;
-    float p[8];
-#pragma unroll
-    for (int x = 0; x < 8; ++x) {
-      p[x] = __builtin_amdgcn_exp2f(fmaf(s[x / 4][x % 4], a.c, -sub));
-      l += p[x];
-    }
+    // Values that are not finite are taken out of the product, and noted for the columns that see them: bit 4 f + x of gone[n] is
+    // o[n][f][x].
+    bool bad = false;
     if constexpr (F32) {
-      bool bad = false;
-      if (masked) {
 #pragma unroll
-        for (int x = 0; x < 8; ++x)
+      for (int x = 0; x < 8; ++x)
 #pragma unroll
-          for (int f = 0; f < F; ++f) bad |= not_finite_f32(t.v[x][f]);
-      }
-      if (masked && __any(bad)) {
-        // values that are not finite are taken out of the product, and set the outputs of the queries that see them
+        for (int f = 0; f < F; ++f) bad |= not_finite_f32(t.v[x][f]);
+      if (__any(bad)) {
 #pragma unroll
-        for (int f = 0; f < F; ++f) {
-          f32x4 marks = f32x4{};
+        for (int n = 0; n < NC; ++n)
 #pragma unroll
-          for (int x = 0; x < 8; ++x) {
-            const bool n = not_finite_f32(t.v[x][f]);
-            o[f] = __builtin_amdgcn_mfma_f32_16x16x4f32(n ? 0.f : t.v[x][f], p[x], o[f], 0, 0, 0);
-            marks = __builtin_amdgcn_mfma_f32_16x16x4f32(n ? 1.f : 0.f, sees[x] ? 1.f : 0.f, marks, 0, 0, 0);
+          for (int f = 0; f < F; ++f) {
+            f32x4 marks = f32x4{};
+#pragma unroll
+            for (int x = 0; x < 8; ++x)
+              marks = __builtin_amdgcn_mfma_f32_16x16x4f32(not_finite_f32(t.v[x][f]) ? 1.f : 0.f, sees(n, x, k0, ok0, ok1, g) ? 1.f : 0.f, marks, 0, 0, 0);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) gone[n] |= marks[x] != 0.f ? 1u << (4 * f + x) : 0u;
           }
 #pragma unroll
-          for (int x = 0; x < 4; ++x)
-            if (marks[x] != 0.f) o[f][x] = NAN;
+        for (int x = 0; x < 8; ++x)
+#pragma unroll
+          for (int f = 0; f < F; ++f) t.v[x][f] = not_finite_f32(t.v[x][f]) ? 0.f : t.v[x][f];
+      }
+      product_f32(t.v, p);
+    } else {
+      uint32_t w[8][D / 32];
+      t.values(w, lane);
+#pragma unroll
+      for (int x = 0; x < 8; ++x)
+#pragma unroll
+        for (int y = 0; y < D / 32; ++y) bad |= not_finite_bf16(w[x][y]);
+      if (__any(bad)) {
+#pragma unroll
+        for (int n = 0; n < NC; ++n) {
+          bf16x8 one;
+#pragma unroll
+          for (int x = 0; x < 8; ++x) one[x] = (__bf16)(sees(n, x, k0, ok0, ok1, g) ? 1.f : 0.f);
+#pragma unroll
+          for (int f = 0; f < F; ++f) {
+            u32x4 mark = turned(w, f / 2, f % 2);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) mark[x] = marks_bf16(mark[x]);
+            const f32x4 marks = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, mark), one, f32x4{}, 0, 0, 0);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) gone[n] |= marks[x] != 0.f ? 1u << (4 * f + x) : 0u;
+          }
         }
-      } else {
 #pragma unroll
         for (int x = 0; x < 8; ++x)
 #pragma unroll
-          for (int f = 0; f < F; ++f) o[f] = __builtin_amdgcn_mfma_f32_16x16x4f32(t.v[x][f], p[x], o[f], 0, 0, 0);
+          for (int y = 0; y < D / 32; ++y) w[x][y] = finite_bf16(w[x][y]);
       }
-    } else {
-      bf16x8 pf[NP];
+      product_bf16(w, p);
+    }
+  }
+
+  __device__ __forceinline__ bool sees(int n, int x, long k0, bool ok0, bool ok1, int g) const {
+    return (x < 4 ? ok0 : ok1) && k0 + 16 * (x / 4) + 4 * g + x % 4 < mine[n];
+  }
+
+  __device__ __forceinline__ void product_f32(const float (&v)[8][F], const float (&p)[NC][8]) {
+#pragma unroll
+    for (int x = 0; x < 8; ++x)
+#pragma unroll
+      for (int f = 0; f < F; ++f)
+#pragma unroll
+        for (int n = 0; n < NC; ++n) o[n][f] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[x][f], p[n][x], o[n][f], 0, 0, 0);
+  }
+  // low (h = 0) or high halves of word y of eight keys: operand 2 y + h
+  static __device__ __forceinline__ u32x4 turned(const uint32_t (&w)[8][D / 32], int y, int h) {
+    u32x4 v;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) v[x] = __builtin_amdgcn_perm(w[2 * x + 1][y], w[2 * x][y], h ? 0x07060302u : 0x05040100u);
+    return v;
+  }
+  __device__ __forceinline__ void product_bf16(const uint32_t (&w)[8][D / 32], const float (&p)[NC][8]) {
+    bf16x8 pf[NC][NP];
+#pragma unroll
+    for (int n = 0; n < NC; ++n)
 #pragma unroll
       for (int x = 0; x < 8; ++x) {
         __bf16 parts[NP];
-        split<NP>(p[x], parts);
+        split<NP>(p[n][x], parts);
 #pragma unroll
-        for (int z = 0; z < NP; ++z) pf[z][x] = parts[z];
+        for (int z = 0; z < NP; ++z) pf[n][z][x] = parts[z];
       }
-      uint32_t w[8][D / 32];
-      t.values(w, lane);
-      bool bad = false;
-      if (masked) {
 #pragma unroll
-        for (int x = 0; x < 8; ++x)
+    for (int f = 0; f < F; ++f) {
+      const bf16x8 v = __builtin_bit_cast(bf16x8, turned(w, f / 2, f % 2));
 #pragma unroll
-          for (int y = 0; y < D / 32; ++y) bad |= not_finite_bf16(w[x][y]);
-      }
-      const bool unusual = masked && __any(bad);
+      for (int n = 0; n < NC; ++n)
 #pragma unroll
-      for (int y = 0; y < D / 32; ++y)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {                            // low and high halves of the words: operand 2 y + h
-          u32x4 v;
-#pragma unroll
-          for (int x = 0; x < 4; ++x) v[x] = __builtin_amdgcn_perm(w[2 * x + 1][y], w[2 * x][y], h ? 0x07060302u : 0x05040100u);
-          const int f = 2 * y + h;
-          if (unusual) {
-            u32x4 mark;
-            bf16x8 one;
-#pragma unroll
-            for (int x = 0; x < 4; ++x) { mark[x] = marks_bf16(v[x]); v[x] = finite_bf16(v[x]); }
-#pragma unroll
-            for (int x = 0; x < 8; ++x) one[x] = (__bf16)(sees[x] ? 1.f : 0.f);
-            const f32x4 marks = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, mark), one, f32x4{}, 0, 0, 0);
-#pragma unroll
-            for (int x = 0; x < 4; ++x)
-              if (marks[x] != 0.f) o[f][x] = NAN;
-          }
-#pragma unroll
-          for (int z = NP - 1; z >= 0; --z)
-            o[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), pf[z], o[f], 0, 0, 0);
-        }
+        for (int z = NP - 1; z >= 0; --z) o[n][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[n][z], o[n][f], 0, 0, 0);
     }
   }
-  l = sum_groups(l);
-  if (g == 0) { ml_lds[wave][r][0] = m; ml_lds[wave][r][1] = l; }
-#pragma unroll
-  for (int x = 0; x < 4; ++x)                                    // accumulator row 4 g + x of operand f: dim F (4 g + x) + f
-#pragma unroll
-    for (int f = 0; f < F; ++f) o_lds[wave][r][F * (4 * g + x) + f] = o[f][x];
-  __syncthreads();
+};
 
-  const int c = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * F;   // 16 threads a column, D / 16 dims each
-  if (col0 + c >= a.cols) return;
-  float top = -INFINITY, total = 0.f, y[F];
-#pragma unroll
-  for (int w = 0; w < 4; ++w) top = fmaxf(top, ml_lds[w][c][0]);
-#pragma unroll
-  for (int f = 0; f < F; ++f) y[f] = 0.f;
-  const float sub = top == -INFINITY ? 0.f : top;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    const float f = __builtin_amdgcn_exp2f(ml_lds[w][c][0] - sub);
-    total = fmaf(ml_lds[w][c][1], f, total);
-#pragma unroll
-    for (int x = 0; x < F; ++x) y[x] = fmaf(o_lds[w][c][d0 + x], f, y[x]);
+template <int D, int HELD, bool QF32, int NP, int NC, typename Out>
+__global__ __launch_bounds__(256, (PagedShape<D, HELD, NC>::WAVES)) void k_paged(PagedArgs a) {
+  constexpr int F = D / 16, OP = D + 4;
+  __shared__ __align__(16) float o_lds[4][16][OP];
+  __shared__ float ml_lds[4][16][2];
+  const int kv = a.cache.kv_heads, ct = (a.cols + 16 * NC - 1) / (16 * NC);
+  const int kvh = blockIdx.x % kv, rest = blockIdx.x / kv, col0 = (rest % ct) * (16 * NC), b = rest / ct, chunk = blockIdx.y;
+  const int len = paged_len(a, b);
+  const int shift = chunk_shift(len, a.cols), chunks = chunks_of(len, a.cols);
+  if (chunk > 0 && chunk >= chunks) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+  const int G = a.heads / kv, per_wave = 1 << (shift - 2);       // keys of a wave
+  const long lo = ((long)chunk << shift) + wave * per_wave, hi = min(lo + per_wave, (long)len);
+  // pages of the wave's keys, 16 a lane: 16 keys lie in one page
+  int pages = 0;
+  if (lo + 16 * lane < hi) {
+    pages = page_of(a.cache, b, (lo + 16 * lane) >> a.cache.page_shift);
+    if (pages < 0) report(a.status, STATUS_PAGE);
   }
-  const int token_c = (col0 + c) / G, head_c = kvh * G + (col0 + c) % G;
-  if (chunks > 1) {
-    const int64_t at_c = (((int64_t)b * kv + kvh) * a.cols + col0 + c) * a.max_chunks + chunk;
+  const long all = seen(col0 / G, a.tokens, len, a.causal);      // keys that every column sees
+  typedef PagedWave<D, HELD, QF32, NP, NC> Wave;
+  typedef typename Wave::Tile Tile;
+  Wave w;
+  const int page_mask = (1 << a.cache.page_shift) - 1;
+  auto load = [&](Tile& t, int n, bool (&ok)[2]) __attribute__((always_inline)) {
+    int64_t row[2];
 #pragma unroll
-    for (int x = 0; x < F; ++x) a.part[at_c * D + d0 + x] = y[x];
-    if (d0 == 0) { a.part_ml[2 * at_c] = top; a.part_ml[2 * at_c + 1] = total; }
-  } else {
-    const int64_t row = (int64_t)b * a.tokens + token_c;
-    Out* out = static_cast<Out*>(a.out) + row * a.out_row + head_c * D + d0;
+    for (int s = 0; s < 2; ++s) {
+      const int page = __builtin_amdgcn_readlane(pages, 2 * n + s);
+      ok[s] = page >= 0;
+      row[s] = pool_row(a.cache, max(page, 0), kvh, (int)((lo + 32 * n + 16 * s) & page_mask));
+    }
+    t.load(a.cache, row, lane);
+  };
+  const int tiles = lo < hi ? (int)((hi - lo + 31) >> 5) : 0;
+  int plain = __any(pages < 0) ? 0 : min(tiles, (int)((max(all - lo, 0L)) >> 5));   // tiles that every column sees in full
+  Tile t[2];
+  bool ok[2];
+  if (tiles > 0) load(t[0], 0, ok);
+  auto clear = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int x = 0; x < F; ++x) out[x] = (Out)(total == 0.f ? 0.f : y[x] / total);
-    if (a.lse && d0 == 0) a.lse[row * a.heads + head_c] = (top + __builtin_amdgcn_logf(total)) * LN2;
+    for (int n = 0; n < NC; ++n) w.clear(n);
+  };
+#pragma unroll
+  for (int n = 0; n < NC; ++n) {
+    const int col = col0 + 16 * n + r, at = min(col, a.cols - 1), token = at / G;
+    w.mine[n] = col < a.cols ? seen(token, a.tokens, len, a.causal) : 0;
+    w.start(n, a.q, ((int64_t)b * a.tokens + token) * a.q_row + (kvh * G + at % G) * D, g);
+  }
+  clear();
+  if (plain > 0) {
+    if constexpr (PagedShape<D, HELD, NC>::AHEAD) {              // the next tile's loads before this one's products
+      if (1 < tiles) load(t[1], 1, ok);
+      w.template step<true>(t[0], a.c, lane);
+      int n = 1;
+      for (; n + 1 < plain; n += 2) {
+        load(t[0], n + 1, ok);
+        w.template step<false>(t[1], a.c, lane);
+        if (n + 2 < tiles) load(t[1], n + 2, ok);
+        w.template step<false>(t[0], a.c, lane);
+      }
+      if (n < plain) {
+        if (n + 1 < tiles) load(t[0], n + 1, ok);
+        w.template step<false>(t[1], a.c, lane);
+      } else if (n < tiles) {
+        t[0] = t[1];
+      }
+    } else {
+      w.template step<true>(t[0], a.c, lane);
+      for (int n = 1; n < plain; ++n) {
+        load(t[0], n, ok);
+        w.template step<false>(t[0], a.c, lane);
+      }
+      if (plain < tiles) load(t[0], plain, ok);
+    }
+    if (w.rose()) {                                              // once more, with maxima that move
+      plain = 0;
+      clear();
+      load(t[0], 0, ok);
+    }
+  }
+  for (int n = plain; n < tiles; ++n) {
+    w.masked_step(t[0], lo + 32 * n, ok[0], ok[1], a.c, lane);
+    if (n + 1 < tiles) load(t[0], n + 1, ok);
+  }
+#pragma unroll
+  for (int n = 0; n < NC; ++n) {
+    const float l = sum_groups(w.l[n]);
+    if (n > 0) __syncthreads();
+    if (g == 0) { ml_lds[wave][r][0] = w.m[n]; ml_lds[wave][r][1] = l; }
+#pragma unroll
+    for (int x = 0; x < 4; ++x)                                  // accumulator row 4 g + x of operand f: dim F (4 g + x) + f
+#pragma unroll
+      for (int f = 0; f < F; ++f) o_lds[wave][r][F * (4 * g + x) + f] = w.gone[n] >> (4 * f + x) & 1 ? NAN : w.o[n][f][x];
+    __syncthreads();
+
+    const int c = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * F, col = col0 + 16 * n + c;   // 16 threads a column, D / 16 dims each
+    if (col >= a.cols) continue;
+    float top = -INFINITY, total = 0.f, y[F];
+#pragma unroll
+    for (int v = 0; v < 4; ++v) top = fmaxf(top, ml_lds[v][c][0]);
+#pragma unroll
+    for (int f = 0; f < F; ++f) y[f] = 0.f;
+    const float sub = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      const float f = __builtin_amdgcn_exp2f(ml_lds[v][c][0] - sub);
+      total = fmaf(ml_lds[v][c][1], f, total);
+#pragma unroll
+      for (int x = 0; x < F; ++x) y[x] = fmaf(o_lds[v][c][d0 + x], f, y[x]);
+    }
+    const int head = kvh * G + col % G;
+    if (chunks > 1) {
+      const int64_t at = (((int64_t)b * kv + kvh) * a.cols + col) * a.max_chunks + chunk;
+#pragma unroll
+      for (int x = 0; x < F; ++x) a.part[at * D + d0 + x] = y[x];
+      if (d0 == 0) { a.part_ml[2 * at] = top; a.part_ml[2 * at + 1] = total; }
+    } else {
+      const int64_t row = (int64_t)b * a.tokens + col / G;
+      Out* out = static_cast<Out*>(a.out) + row * a.out_row + head * D + d0;
+#pragma unroll
+      for (int x = 0; x < F; ++x) out[x] = (Out)(total == 0.f ? 0.f : y[x] / total);
+      if (a.lse && d0 == 0) a.lse[row * a.heads + head] = (top + __builtin_amdgcn_logf(total)) * LN2;
+    }
   }
 }
 

@@ -65,10 +65,6 @@ __device__ __forceinline__ void to_lds(const void* g, void* lds) {
 template <int CH> __device__ __forceinline__ int key_swizzle(int row) { return CH >= 16 ? row & 15 : CH == 8 ? (row >> 1) & 7 : (row >> 2) & 3; }
 template <int CH> __device__ __forceinline__ int value_swizzle(int row) { return CH >= 16 ? (row & 3) << 2 : CH == 8 ? ((row >> 1) & 1) << 2 : 0; }
 
-// The maximum m_i is that of the first 32 keys, and moves only where a score is 2^48 times its weight above it (each query by
-// its own scores): weights up to 2^48 lose nothing in floating types, and leave 2^59 to the values before a sum of 2^20 of
-// them overflows.
-constexpr float MOST_RISE = 48.f;
 constexpr int VM_NONE = 0x0F70;              // s_waitcnt vmcnt(0)
 
 // bf16.  A wave owns 32 queries.  Keys go by 32 (half a tile) through three stages that do not depend on each other and are
@@ -296,7 +292,7 @@ __global__ __launch_bounds__(NW * 64, WAVES) void k_prompt_bf16(PromptArgs a) {
 #undef TSDP_FIRST
 #undef TSDP_SECOND
 #undef TSDP_MIDDLE
-    if (__any(w.l > __builtin_amdgcn_exp2f(MOST_RISE)) && lane == 0) rises[wave] = 1;   // some weight was more, or infinite
+    if (__any(w.l > most_sum(w.m)) && lane == 0) rises[wave] = 1;
     __syncthreads();
     from = full;
     if (any_of<NW>(rises)) {                 // once more from the start
