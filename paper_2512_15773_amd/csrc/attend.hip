@@ -10,6 +10,7 @@
 #include "cache_kernels.hpp"
 #include "attend_prompt.hpp"
 #include "attend_paged.hpp"
+#include "attend_wide.hpp"
 
 using namespace tsdp;
 
@@ -75,8 +76,8 @@ dim3 prompt_grid(PromptArgs& a) {
 template <int D>
 void launch_prompt(int type, PromptArgs a, hipStream_t s) {
   if (type == 0) {
-    const dim3 grid = prompt_grid<128>(a);
-    hipLaunchKernelGGL((k_prompt_f32<D, 4>), grid, dim3(256), 0, s, a);
+    const dim3 grid = prompt_grid<64>(a);
+    hipLaunchKernelGGL((k_wide<D, HELD_F32, true, 3, float, false, PromptArgs>), grid, dim3(256), 0, s, a);
     return;
   }
   // Sequences of at most 320 keys on average: three waves a SIMD instead of the overlapped loop (256 of 96 tokens, 8 heads of
@@ -92,23 +93,23 @@ void launch_prompt(int type, PromptArgs a, hipStream_t s) {
   hipLaunchKernelGGL((k_prompt_bf16<D, 4, 2, true>), grid, dim3(256), 0, s, a);
 }
 
-template <int D, int HELD, bool QF32, int NP, int NC, typename Out>
-void launch_paged_tiles(const PagedArgs& a, hipStream_t s) {
-  const int ct = (a.cols + 16 * NC - 1) / (16 * NC);
-  hipLaunchKernelGGL((k_paged<D, HELD, QF32, NP, NC, Out>), dim3((unsigned)((int64_t)a.B * ct * a.cache.kv_heads), a.max_chunks), dim3(256), 0, s, a);
-}
 template <int D, int HELD, bool QF32, int NP, typename Out>
 void launch_paged(const PagedArgs& a, hipStream_t s) {
-  constexpr int MOST = HELD == HELD_F32 || QF32 ? 1 : D == 128 ? 2 : 4;
-  if (MOST > 1 && a.cols > 16) launch_paged_tiles<D, HELD, QF32, NP, MOST, Out>(a, s);
-  else launch_paged_tiles<D, HELD, QF32, NP, 1, Out>(a, s);
-  if (a.max_chunks > 1)
-    hipLaunchKernelGGL((k_paged_join<D, Out>), dim3((unsigned)((int64_t)a.B * a.cache.kv_heads * a.cols)), dim3(256), 0, s, a);
+  const int64_t bk = (int64_t)a.B * a.cache.kv_heads;
+  if (a.cols <= 16)
+    hipLaunchKernelGGL((k_paged<D, HELD, QF32, NP, Out>), dim3((unsigned)bk, a.max_chunks), dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((k_wide<D, HELD, QF32, NP, Out, true, PagedArgs>), dim3((unsigned)(bk * ((a.cols + 63) / 64)), a.max_chunks), dim3(256), 0, s, a);
+  if (a.max_chunks <= 1) return;
+  if (a.max_chunks <= JOIN_ONE)
+    hipLaunchKernelGGL((k_paged_join<D, Out, 4>), dim3((unsigned)((int64_t)a.B * a.cache.kv_heads * ((a.cols + 3) / 4))), dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((k_paged_join<D, Out, 1>), dim3((unsigned)((int64_t)a.B * a.cache.kv_heads * a.cols)), dim3(256), 0, s, a);
 }
 
 template <int D>
 void launch_paged_held(int held, int type, int out_type, const PagedArgs& a, hipStream_t s) {
-  if (held == 0) launch_paged<D, HELD_F32, true, 1, float>(a, s);
+  if (held == 0) launch_paged<D, HELD_F32, true, 3, float>(a, s);
   else if (held == 1 && out_type == 0) launch_paged<D, HELD_BF16, false, 3, float>(a, s);
   else if (held == 1) launch_paged<D, HELD_BF16, false, 2, __bf16>(a, s);
   else if (type == 0) launch_paged<D, HELD_MX8, true, 3, float>(a, s);

@@ -39,14 +39,6 @@ __device__ __forceinline__ int paged_len(const PagedArgs& a, int b) {
 
 template <int D, int HELD> struct PagedTile;
 
-// AHEAD: registers hold two tiles; WAVES: waves a SIMD that they leave room for
-#ifndef PWV
-#define PWV 2
-#endif
-template <int D, int HELD, int NC> struct PagedShape {
-  static constexpr bool AHEAD = !(HELD == HELD_F32 && D == 128);
-  static constexpr int WAVES = PWV;
-};
 
 template <int D> struct PagedTile<D, HELD_BF16> {
   u32x4 k[2][D / 32];
@@ -143,34 +135,36 @@ template <int D> struct PagedTile<D, HELD_F32> {
   }
 };
 
-// x as NP bf16 parts whose sum it is to 2^-8 (1), 2^-16 (2), 2^-24 (3) of it
+// x as NP bf16 parts whose sum it is to 2^-8 (1), 2^-16 (2), 2^-24 (3) of it; an infinity has parts that are NaN
 template <int NP>
-__device__ __forceinline__ void split(float x, __bf16 (&p)[NP]) {
+__device__ __forceinline__ void split(float x, float y, bf16x2 (&p)[NP]) {
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
-    p[i] = (__bf16)x;
-    x = not_finite_f32(x) ? 0.f : x - (float)p[i];
+    p[i] = bf16x2{(__bf16)x, (__bf16)y};
+    const uint32_t w = __builtin_bit_cast(uint32_t, p[i]);
+    x -= as_f32(w << 16);
+    y -= as_f32(w & 0xFFFF0000u);
   }
 }
 
-// One wave's share: NC tiles of 16 columns, a running softmax for each.
+// One wave's share: 16 columns, with a softmax of their own.
 // QF32: queries are fp32.  NP: bf16 parts of P (unused where the cache is fp32).
-template <int D, int HELD, bool QF32, int NP, int NC>
+template <int D, int HELD, bool QF32, int NP>
 struct PagedWave {
   static constexpr bool F32 = HELD == HELD_F32;
   static constexpr int NQ = QF32 && !F32 ? 3 : 1, F = D / 16;
   typedef PagedTile<D, HELD> Tile;
-  bf16x8 q[NC][F32 ? 1 : NQ][F32 ? 1 : D / 32];
-  f32x4 qx[NC][F32 ? F : 1];
-  f32x4 o[NC][F];
-  float m[NC], l[NC];
-  int mine[NC];                              // keys that this lane's column sees
-  uint32_t gone[NC];                         // outputs that a visible value makes NaN
+  bf16x8 q[F32 ? 1 : NQ][F32 ? 1 : D / 32];
+  f32x4 qx[F32 ? F : 1];
+  f32x4 o[F];
+  float m, l;
+  int mine;                                  // keys that this lane's column sees
+  uint32_t gone;                             // outputs that a visible value makes NaN: bit 4 f + x is o[f][x]
 
-  __device__ __forceinline__ void start(int n, const void* at, int64_t off, int g) {
+  __device__ __forceinline__ void start(const void* at, int64_t off, int g) {
     if constexpr (F32) {
 #pragma unroll
-      for (int x = 0; x < F; ++x) qx[n][x] = *reinterpret_cast<const f32x4*>(static_cast<const float*>(at) + off + 16 * x + 4 * g);
+      for (int x = 0; x < F; ++x) qx[x] = *reinterpret_cast<const f32x4*>(static_cast<const float*>(at) + off + 16 * x + 4 * g);
     } else {
 #pragma unroll
       for (int x = 0; x < D / 32; ++x) {
@@ -178,25 +172,25 @@ struct PagedWave {
         if constexpr (QF32) {
           const float* p = static_cast<const float*>(at) + off + d;
 #pragma unroll
-          for (int y = 0; y < 8; ++y) {
-            __bf16 parts[3];
-            split<3>(p[y], parts);
+          for (int y = 0; y < 8; y += 2) {
+            bf16x2 parts[3];
+            split<3>(p[y], p[y + 1], parts);
 #pragma unroll
-            for (int z = 0; z < 3; ++z) q[n][z][x][y] = parts[z];
+            for (int z = 0; z < 3; ++z) { q[z][x][y] = parts[z][0]; q[z][x][y + 1] = parts[z][1]; }
           }
         } else {
-          q[n][0][x] = *reinterpret_cast<const bf16x8*>(static_cast<const __bf16*>(at) + off + d);
+          q[0][x] = *reinterpret_cast<const bf16x8*>(static_cast<const __bf16*>(at) + off + d);
         }
       }
     }
   }
-  __device__ __forceinline__ void clear(int n) {
+  __device__ __forceinline__ void clear() {
 #pragma unroll
-    for (int f = 0; f < F; ++f) o[n][f] = f32x4{};
-    m[n] = -INFINITY; l[n] = 0.f; gone[n] = 0;
+    for (int f = 0; f < F; ++f) o[f] = f32x4{};
+    m = -INFINITY; l = 0.f; gone = 0;
   }
 
-  __device__ __forceinline__ void scores(const Tile& t, int n, f32x4 (&s)[2], int lane) const {
+  __device__ __forceinline__ void scores(const Tile& t, f32x4 (&s)[2], int lane) const {
     s[0] = f32x4{}; s[1] = f32x4{};
     if constexpr (F32) {
 #pragma unroll
@@ -204,7 +198,7 @@ struct PagedWave {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
-          for (int u = 0; u < 2; ++u) s[u] = __builtin_amdgcn_mfma_f32_16x16x4f32(t.k[u][x][j], qx[n][x][j], s[u], 0, 0, 0);
+          for (int u = 0; u < 2; ++u) s[u] = __builtin_amdgcn_mfma_f32_16x16x4f32(t.k[u][x][j], qx[x][j], s[u], 0, 0, 0);
     } else {
 #pragma unroll
       for (int x = 0; x < D / 32; ++x)
@@ -212,7 +206,7 @@ struct PagedWave {
         for (int u = 0; u < 2; ++u) {
           const bf16x8 key = t.key(u, x, lane);
 #pragma unroll
-          for (int z = NQ - 1; z >= 0; --z) s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q[n][z][x], s[u], 0, 0, 0);
+          for (int z = NQ - 1; z >= 0; --z) s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q[z][x], s[u], 0, 0, 0);
         }
     }
   }
@@ -220,29 +214,26 @@ struct PagedWave {
     const float top = max3(max3(s[0][0], s[0][1], s[0][2]), s[0][3], s[1][0]);
     return max_groups(max3(max3(top, s[1][1], s[1][2]), s[1][3], s[1][3]));
   }
-  __device__ __forceinline__ void weights(const f32x4 (&s)[2], int n, float c, float (&p)[8]) {
-    const float sub = m[n] == -INFINITY ? 0.f : m[n];
+  __device__ __forceinline__ void weights(const f32x4 (&s)[2], float c, float (&p)[8]) {
+    const float sub = m == -INFINITY ? 0.f : m;
 #pragma unroll
     for (int x = 0; x < 8; ++x) {
       p[x] = __builtin_amdgcn_exp2f(fmaf(s[x / 4][x % 4], c, -sub));
-      l[n] += p[x];
+      l += p[x];
     }
   }
 
   // 32 keys that every column sees.  FIRST: their maximum is taken; afterwards it stays, and a rise above it shows in the sums.
   template <bool FIRST>
   __device__ __forceinline__ void step(const Tile& t, float c, int lane) {
-    float p[NC][8];
-#pragma unroll
-    for (int n = 0; n < NC; ++n) {
-      f32x4 s[2];
-      scores(t, n, s, lane);
-      if (FIRST) {
-        const float top = largest(s) * c;
-        m[n] = top > -INFINITY ? top : -INFINITY;
-      }
-      weights(s, n, c, p[n]);
+    float p[8];
+    f32x4 s[2];
+    scores(t, s, lane);
+    if (FIRST) {
+      const float top = largest(s) * c;
+      m = top > -INFINITY ? top : -INFINITY;
     }
+    weights(s, c, p);
     if constexpr (F32) {
       product_f32(t.v, p);
     } else {
@@ -251,35 +242,26 @@ struct PagedWave {
       product_bf16(w, p);
     }
   }
-  __device__ __forceinline__ bool rose() const {
-    bool r = false;
-#pragma unroll
-    for (int n = 0; n < NC; ++n) r |= l[n] > most_sum(m[n]);
-    return __any(r);
-  }
+  __device__ __forceinline__ bool rose() const { return __any(l > most_sum(m)); }
 
   // Any 32 keys from position k0 on.  ok: their halves' pages are inside the pool.
   __device__ __forceinline__ void masked_step(Tile& t, long k0, bool ok0, bool ok1, float c, int lane) {
     const int g = lane >> 4;
-    float p[NC][8];
+    float p[8];
+    f32x4 s[2];
+    scores(t, s, lane);
 #pragma unroll
-    for (int n = 0; n < NC; ++n) {
-      f32x4 s[2];
-      scores(t, n, s, lane);
+    for (int x = 0; x < 8; ++x)
+      if (!sees(x, k0, ok0, ok1, g)) s[x / 4][x % 4] = -INFINITY;
+    const float top = largest(s) * c, to = top > m + MOST_RISE ? top : m, by = to == m ? 1.f : __builtin_amdgcn_exp2f(m - to);
+    m = to;
+    l *= by;
 #pragma unroll
-      for (int x = 0; x < 8; ++x)
-        if (!sees(n, x, k0, ok0, ok1, g)) s[x / 4][x % 4] = -INFINITY;
-      const float top = largest(s) * c, to = top > m[n] + MOST_RISE ? top : m[n], f = to == m[n] ? 1.f : __builtin_amdgcn_exp2f(m[n] - to);
-      m[n] = to;
-      l[n] *= f;
+    for (int y = 0; y < F; ++y)
 #pragma unroll
-      for (int y = 0; y < F; ++y)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) o[n][y][x] *= f;
-      weights(s, n, c, p[n]);
-    }
-    // Values that are not finite are taken out of the product, and noted for the columns that see them: bit 4 f + x of gone[n] is
-    // o[n][f][x].
+      for (int x = 0; x < 4; ++x) o[y][x] *= by;
+    weights(s, c, p);
+    // Values that are not finite are taken out of the product, and noted for the columns that see them.
     bool bad = false;
     if constexpr (F32) {
 #pragma unroll
@@ -288,16 +270,14 @@ struct PagedWave {
         for (int f = 0; f < F; ++f) bad |= not_finite_f32(t.v[x][f]);
       if (__any(bad)) {
 #pragma unroll
-        for (int n = 0; n < NC; ++n)
+        for (int f = 0; f < F; ++f) {
+          f32x4 marks = f32x4{};
 #pragma unroll
-          for (int f = 0; f < F; ++f) {
-            f32x4 marks = f32x4{};
+          for (int x = 0; x < 8; ++x)
+            marks = __builtin_amdgcn_mfma_f32_16x16x4f32(not_finite_f32(t.v[x][f]) ? 1.f : 0.f, sees(x, k0, ok0, ok1, g) ? 1.f : 0.f, marks, 0, 0, 0);
 #pragma unroll
-            for (int x = 0; x < 8; ++x)
-              marks = __builtin_amdgcn_mfma_f32_16x16x4f32(not_finite_f32(t.v[x][f]) ? 1.f : 0.f, sees(n, x, k0, ok0, ok1, g) ? 1.f : 0.f, marks, 0, 0, 0);
-#pragma unroll
-            for (int x = 0; x < 4; ++x) gone[n] |= marks[x] != 0.f ? 1u << (4 * f + x) : 0u;
-          }
+          for (int x = 0; x < 4; ++x) gone |= marks[x] != 0.f ? 1u << (4 * f + x) : 0u;
+        }
 #pragma unroll
         for (int x = 0; x < 8; ++x)
 #pragma unroll
@@ -312,20 +292,17 @@ struct PagedWave {
 #pragma unroll
         for (int y = 0; y < D / 32; ++y) bad |= not_finite_bf16(w[x][y]);
       if (__any(bad)) {
+        bf16x8 one;
 #pragma unroll
-        for (int n = 0; n < NC; ++n) {
-          bf16x8 one;
+        for (int x = 0; x < 8; ++x) one[x] = (__bf16)(sees(x, k0, ok0, ok1, g) ? 1.f : 0.f);
 #pragma unroll
-          for (int x = 0; x < 8; ++x) one[x] = (__bf16)(sees(n, x, k0, ok0, ok1, g) ? 1.f : 0.f);
+        for (int f = 0; f < F; ++f) {
+          u32x4 mark = turned(w, f / 2, f % 2);
 #pragma unroll
-          for (int f = 0; f < F; ++f) {
-            u32x4 mark = turned(w, f / 2, f % 2);
+          for (int x = 0; x < 4; ++x) mark[x] = marks_bf16(mark[x]);
+          const f32x4 marks = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, mark), one, f32x4{}, 0, 0, 0);
 #pragma unroll
-            for (int x = 0; x < 4; ++x) mark[x] = marks_bf16(mark[x]);
-            const f32x4 marks = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, mark), one, f32x4{}, 0, 0, 0);
-#pragma unroll
-            for (int x = 0; x < 4; ++x) gone[n] |= marks[x] != 0.f ? 1u << (4 * f + x) : 0u;
-          }
+          for (int x = 0; x < 4; ++x) gone |= marks[x] != 0.f ? 1u << (4 * f + x) : 0u;
         }
 #pragma unroll
         for (int x = 0; x < 8; ++x)
@@ -336,17 +313,15 @@ struct PagedWave {
     }
   }
 
-  __device__ __forceinline__ bool sees(int n, int x, long k0, bool ok0, bool ok1, int g) const {
-    return (x < 4 ? ok0 : ok1) && k0 + 16 * (x / 4) + 4 * g + x % 4 < mine[n];
+  __device__ __forceinline__ bool sees(int x, long k0, bool ok0, bool ok1, int g) const {
+    return (x < 4 ? ok0 : ok1) && k0 + 16 * (x / 4) + 4 * g + x % 4 < mine;
   }
 
-  __device__ __forceinline__ void product_f32(const float (&v)[8][F], const float (&p)[NC][8]) {
+  __device__ __forceinline__ void product_f32(const float (&v)[8][F], const float (&p)[8]) {
 #pragma unroll
     for (int x = 0; x < 8; ++x)
 #pragma unroll
-      for (int f = 0; f < F; ++f)
-#pragma unroll
-        for (int n = 0; n < NC; ++n) o[n][f] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[x][f], p[n][x], o[n][f], 0, 0, 0);
+      for (int f = 0; f < F; ++f) o[f] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[x][f], p[x], o[f], 0, 0, 0);
   }
   // low (h = 0) or high halves of word y of eight keys: operand 2 y + h
   static __device__ __forceinline__ u32x4 turned(const uint32_t (&w)[8][D / 32], int y, int h) {
@@ -355,35 +330,31 @@ struct PagedWave {
     for (int x = 0; x < 4; ++x) v[x] = __builtin_amdgcn_perm(w[2 * x + 1][y], w[2 * x][y], h ? 0x07060302u : 0x05040100u);
     return v;
   }
-  __device__ __forceinline__ void product_bf16(const uint32_t (&w)[8][D / 32], const float (&p)[NC][8]) {
-    bf16x8 pf[NC][NP];
+  __device__ __forceinline__ void product_bf16(const uint32_t (&w)[8][D / 32], const float (&p)[8]) {
+    bf16x8 pf[NP];
 #pragma unroll
-    for (int n = 0; n < NC; ++n)
+    for (int x = 0; x < 8; x += 2) {
+      bf16x2 parts[NP];
+      split<NP>(p[x], p[x + 1], parts);
 #pragma unroll
-      for (int x = 0; x < 8; ++x) {
-        __bf16 parts[NP];
-        split<NP>(p[n][x], parts);
-#pragma unroll
-        for (int z = 0; z < NP; ++z) pf[n][z][x] = parts[z];
-      }
+      for (int z = 0; z < NP; ++z) { pf[z][x] = parts[z][0]; pf[z][x + 1] = parts[z][1]; }
+    }
 #pragma unroll
     for (int f = 0; f < F; ++f) {
       const bf16x8 v = __builtin_bit_cast(bf16x8, turned(w, f / 2, f % 2));
 #pragma unroll
-      for (int n = 0; n < NC; ++n)
-#pragma unroll
-        for (int z = NP - 1; z >= 0; --z) o[n][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[n][z], o[n][f], 0, 0, 0);
+      for (int z = NP - 1; z >= 0; --z) o[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[z], o[f], 0, 0, 0);
     }
   }
 };
 
-template <int D, int HELD, bool QF32, int NP, int NC, typename Out>
-__global__ __launch_bounds__(256, (PagedShape<D, HELD, NC>::WAVES)) void k_paged(PagedArgs a) {
+template <int D, int HELD, bool QF32, int NP, typename Out>
+__global__ __launch_bounds__(256, 2) void k_paged(PagedArgs a) {
   constexpr int F = D / 16, OP = D + 4;
+  constexpr bool AHEAD = !(HELD == HELD_F32 && D == 128);        // registers hold two tiles
   __shared__ __align__(16) float o_lds[4][16][OP];
   __shared__ float ml_lds[4][16][2];
-  const int kv = a.cache.kv_heads, ct = (a.cols + 16 * NC - 1) / (16 * NC);
-  const int kvh = blockIdx.x % kv, rest = blockIdx.x / kv, col0 = (rest % ct) * (16 * NC), b = rest / ct, chunk = blockIdx.y;
+  const int kv = a.cache.kv_heads, kvh = blockIdx.x % kv, b = blockIdx.x / kv, chunk = blockIdx.y;
   const int len = paged_len(a, b);
   const int shift = chunk_shift(len, a.cols), chunks = chunks_of(len, a.cols);
   if (chunk > 0 && chunk >= chunks) return;
@@ -396,12 +367,13 @@ __global__ __launch_bounds__(256, (PagedShape<D, HELD, NC>::WAVES)) void k_paged
     pages = page_of(a.cache, b, (lo + 16 * lane) >> a.cache.page_shift);
     if (pages < 0) report(a.status, STATUS_PAGE);
   }
-  const long all = seen(col0 / G, a.tokens, len, a.causal);      // keys that every column sees
-  typedef PagedWave<D, HELD, QF32, NP, NC> Wave;
+  const long all = seen(0, a.tokens, len, a.causal);             // keys that every column sees
+  typedef PagedWave<D, HELD, QF32, NP> Wave;
   typedef typename Wave::Tile Tile;
   Wave w;
   const int page_mask = (1 << a.cache.page_shift) - 1;
-  auto load = [&](Tile& t, int n, bool (&ok)[2]) __attribute__((always_inline)) {
+  bool ok[2];                                // the pages of the halves of the tile loaded last are inside the pool
+  auto load = [&](Tile& t, int n) __attribute__((always_inline)) {
     int64_t row[2];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
@@ -414,32 +386,24 @@ __global__ __launch_bounds__(256, (PagedShape<D, HELD, NC>::WAVES)) void k_paged
   const int tiles = lo < hi ? (int)((hi - lo + 31) >> 5) : 0;
   int plain = __any(pages < 0) ? 0 : min(tiles, (int)((max(all - lo, 0L)) >> 5));   // tiles that every column sees in full
   Tile t[2];
-  bool ok[2];
-  if (tiles > 0) load(t[0], 0, ok);
-  auto clear = [&]() __attribute__((always_inline)) {
-#pragma unroll
-    for (int n = 0; n < NC; ++n) w.clear(n);
-  };
-#pragma unroll
-  for (int n = 0; n < NC; ++n) {
-    const int col = col0 + 16 * n + r, at = min(col, a.cols - 1), token = at / G;
-    w.mine[n] = col < a.cols ? seen(token, a.tokens, len, a.causal) : 0;
-    w.start(n, a.q, ((int64_t)b * a.tokens + token) * a.q_row + (kvh * G + at % G) * D, g);
-  }
-  clear();
+  if (tiles > 0) load(t[0], 0);
+  const int at = min(r, a.cols - 1), token = at / G;
+  w.mine = r < a.cols ? seen(token, a.tokens, len, a.causal) : 0;
+  w.start(a.q, ((int64_t)b * a.tokens + token) * a.q_row + (kvh * G + at % G) * D, g);
+  w.clear();
   if (plain > 0) {
-    if constexpr (PagedShape<D, HELD, NC>::AHEAD) {              // the next tile's loads before this one's products
-      if (1 < tiles) load(t[1], 1, ok);
+    if constexpr (AHEAD) {                   // the next tile's loads before this one's products
+      if (1 < tiles) load(t[1], 1);
       w.template step<true>(t[0], a.c, lane);
       int n = 1;
       for (; n + 1 < plain; n += 2) {
-        load(t[0], n + 1, ok);
+        load(t[0], n + 1);
         w.template step<false>(t[1], a.c, lane);
-        if (n + 2 < tiles) load(t[1], n + 2, ok);
+        if (n + 2 < tiles) load(t[1], n + 2);
         w.template step<false>(t[0], a.c, lane);
       }
       if (n < plain) {
-        if (n + 1 < tiles) load(t[0], n + 1, ok);
+        if (n + 1 < tiles) load(t[0], n + 1);
         w.template step<false>(t[1], a.c, lane);
       } else if (n < tiles) {
         t[0] = t[1];
@@ -447,104 +411,125 @@ __global__ __launch_bounds__(256, (PagedShape<D, HELD, NC>::WAVES)) void k_paged
     } else {
       w.template step<true>(t[0], a.c, lane);
       for (int n = 1; n < plain; ++n) {
-        load(t[0], n, ok);
+        load(t[0], n);
         w.template step<false>(t[0], a.c, lane);
       }
-      if (plain < tiles) load(t[0], plain, ok);
+      if (plain < tiles) load(t[0], plain);
     }
-    if (w.rose()) {                                              // once more, with maxima that move
+    if (w.rose()) {                          // once more, with maxima that move
       plain = 0;
-      clear();
-      load(t[0], 0, ok);
+      w.clear();
+      load(t[0], 0);
     }
   }
   for (int n = plain; n < tiles; ++n) {
     w.masked_step(t[0], lo + 32 * n, ok[0], ok[1], a.c, lane);
-    if (n + 1 < tiles) load(t[0], n + 1, ok);
+    if (n + 1 < tiles) load(t[0], n + 1);
   }
+  const float l = sum_groups(w.l);
+  if (g == 0) { ml_lds[wave][r][0] = w.m; ml_lds[wave][r][1] = l; }
 #pragma unroll
-  for (int n = 0; n < NC; ++n) {
-    const float l = sum_groups(w.l[n]);
-    if (n > 0) __syncthreads();
-    if (g == 0) { ml_lds[wave][r][0] = w.m[n]; ml_lds[wave][r][1] = l; }
+  for (int x = 0; x < 4; ++x)                                    // accumulator row 4 g + x of operand f: dim F (4 g + x) + f
 #pragma unroll
-    for (int x = 0; x < 4; ++x)                                  // accumulator row 4 g + x of operand f: dim F (4 g + x) + f
-#pragma unroll
-      for (int f = 0; f < F; ++f) o_lds[wave][r][F * (4 * g + x) + f] = w.gone[n] >> (4 * f + x) & 1 ? NAN : w.o[n][f][x];
-    __syncthreads();
+    for (int f = 0; f < F; ++f) o_lds[wave][r][F * (4 * g + x) + f] = w.gone >> (4 * f + x) & 1 ? NAN : w.o[f][x];
+  __syncthreads();
 
-    const int c = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * F, col = col0 + 16 * n + c;   // 16 threads a column, D / 16 dims each
-    if (col >= a.cols) continue;
-    float top = -INFINITY, total = 0.f, y[F];
+  const int col = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * F; // 16 threads a column, D / 16 dims each
+  if (col >= a.cols) return;
+  float top = -INFINITY, total = 0.f, y[F];
 #pragma unroll
-    for (int v = 0; v < 4; ++v) top = fmaxf(top, ml_lds[v][c][0]);
+  for (int v = 0; v < 4; ++v) top = fmaxf(top, ml_lds[v][col][0]);
 #pragma unroll
-    for (int f = 0; f < F; ++f) y[f] = 0.f;
-    const float sub = top == -INFINITY ? 0.f : top;
+  for (int f = 0; f < F; ++f) y[f] = 0.f;
+  const float sub = top == -INFINITY ? 0.f : top;
 #pragma unroll
-    for (int v = 0; v < 4; ++v) {
-      const float f = __builtin_amdgcn_exp2f(ml_lds[v][c][0] - sub);
-      total = fmaf(ml_lds[v][c][1], f, total);
+  for (int v = 0; v < 4; ++v) {
+    const float f = __builtin_amdgcn_exp2f(ml_lds[v][col][0] - sub);
+    total = fmaf(ml_lds[v][col][1], f, total);
 #pragma unroll
-      for (int x = 0; x < F; ++x) y[x] = fmaf(o_lds[v][c][d0 + x], f, y[x]);
-    }
-    const int head = kvh * G + col % G;
-    if (chunks > 1) {
-      const int64_t at = (((int64_t)b * kv + kvh) * a.cols + col) * a.max_chunks + chunk;
+    for (int x = 0; x < F; ++x) y[x] = fmaf(o_lds[v][col][d0 + x], f, y[x]);
+  }
+  const int head = kvh * G + col % G;
+  if (chunks > 1) {
+    const int64_t place = (((int64_t)b * kv + kvh) * a.cols + col) * a.max_chunks + chunk;
 #pragma unroll
-      for (int x = 0; x < F; ++x) a.part[at * D + d0 + x] = y[x];
-      if (d0 == 0) { a.part_ml[2 * at] = top; a.part_ml[2 * at + 1] = total; }
-    } else {
-      const int64_t row = (int64_t)b * a.tokens + col / G;
-      Out* out = static_cast<Out*>(a.out) + row * a.out_row + head * D + d0;
+    for (int x = 0; x < F; ++x) a.part[place * D + d0 + x] = y[x];
+    if (d0 == 0) { a.part_ml[2 * place] = top; a.part_ml[2 * place + 1] = total; }
+  } else {
+    const int64_t row = (int64_t)b * a.tokens + col / G;
+    Out* out = static_cast<Out*>(a.out) + row * a.out_row + head * D + d0;
 #pragma unroll
-      for (int x = 0; x < F; ++x) out[x] = (Out)(total == 0.f ? 0.f : y[x] / total);
-      if (a.lse && d0 == 0) a.lse[row * a.heads + head] = (top + __builtin_amdgcn_logf(total)) * LN2;
-    }
+    for (int x = 0; x < F; ++x) out[x] = (Out)(total == 0.f ? 0.f : y[x] / total);
+    if (a.lse && d0 == 0) a.lse[row * a.heads + head] = (top + __builtin_amdgcn_logf(total)) * LN2;
   }
 }
 
-// One workgroup adds up the chunks of one column, each of its four waves every fourth one.
-template <int D, typename Out>
-__global__ __launch_bounds__(256) void k_paged_join(PagedArgs a) {
-  constexpr int E = D >= 64 ? D / 64 : 1;                        // dims of a lane
-  __shared__ float o_lds[4][D];
-  __shared__ float ml_lds[4];
-  const int col = blockIdx.x % a.cols, kvh = blockIdx.x / a.cols % a.cache.kv_heads, b = blockIdx.x / a.cols / a.cache.kv_heads;
-  const int len = paged_len(a, b), chunks = chunks_of(len, a.cols);
-  if (chunks <= 1) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, d0 = lane * E;
-  const int64_t at = (((int64_t)b * a.cache.kv_heads + kvh) * a.cols + col) * a.max_chunks;
-  const float* ml = a.part_ml + 2 * at;
-  float top = -INFINITY;
-  for (int n = lane; n < chunks; n += 64) top = fmaxf(top, ml[2 * n]);
+// Adds up the chunks of a column, 16 bytes a lane: D / 4 lanes hold an output, and the lanes of a wave (up to JOIN_ONE chunks) or
+// of four waves (more) so many chunks at a time.  Which, goes by the sequence's own length.
+constexpr int JOIN_ONE = 16;
+template <int D>
+struct PagedJoin {
+  static constexpr int LANES = D / 4, SETS = 64 / LANES;         // chunks that a wave's load covers
+  f32x4 y = f32x4{};
+  float top = -INFINITY, total = 0.f;
+  // chunks first, first + step .. of those at `at`
+  __device__ __forceinline__ void add(const PagedArgs& a, int64_t at, int chunks, int first, int step, int lane) {
+    const float* ml = a.part_ml + 2 * at;
+    for (int n = lane; n < chunks; n += 64) top = fmaxf(top, ml[2 * n]);
 #pragma unroll
-  for (int s = 32; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor(top, s));
-  const float sub = top == -INFINITY ? 0.f : top;
-  float y[E], total = 0.f;
+    for (int s = 32; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor(top, s));
+    const float sub = top == -INFINITY ? 0.f : top;
+    const float* p = a.part + at * D + (lane % LANES) * 4;
+#pragma unroll 4
+    for (int n = first + lane / LANES; n < chunks; n += step) {
+      const float f = __builtin_amdgcn_exp2f(ml[2 * n] - sub);
+      const f32x4 v = *reinterpret_cast<const f32x4*>(p + (int64_t)n * D);
+      total = fmaf(ml[2 * n + 1], f, total);
 #pragma unroll
-  for (int e = 0; e < E; ++e) y[e] = 0.f;
-  for (int n = wave; n < chunks; n += 4) {
-    const float f = __builtin_amdgcn_exp2f(ml[2 * n] - sub);
-    total = fmaf(ml[2 * n + 1], f, total);
-    if (d0 < D) {
+      for (int e = 0; e < 4; ++e) y[e] = fmaf(v[e], f, y[e]);
+    }
 #pragma unroll
-      for (int e = 0; e < E; ++e) y[e] = fmaf(a.part[(at + n) * D + d0 + e], f, y[e]);
+    for (int s = 32; s >= LANES; s >>= 1) {
+      total += __shfl_xor(total, s);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] += __shfl_xor(y[e], s);
     }
   }
-  if (lane == 0) ml_lds[wave] = total;
-  if (d0 < D) {
-#pragma unroll
-    for (int e = 0; e < E; ++e) o_lds[wave][d0 + e] = y[e];
+};
+
+// PER columns a workgroup: four where no sequence of the call can have more than JOIN_ONE chunks.
+template <int D, typename Out, int PER>
+__global__ __launch_bounds__(256) void k_paged_join(PagedArgs a) {
+  typedef PagedJoin<D> Join;
+  __shared__ __align__(16) float lds[4][D + 4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, G = a.heads / a.cache.kv_heads, kv = a.cache.kv_heads;
+  const int groups = (a.cols + PER - 1) / PER, kvh = blockIdx.x / groups % kv, b = blockIdx.x / groups / kv;
+  const int len = paged_len(a, b), chunks = chunks_of(len, a.cols);
+  const bool alone = PER == 4 || chunks <= JOIN_ONE;
+  const int col = blockIdx.x % groups * PER + (PER == 4 ? wave : 0);
+  if (chunks <= 1 || col >= a.cols || (PER == 1 && alone && wave > 0)) return;
+  const int64_t at = (((int64_t)b * kv + kvh) * a.cols + col) * a.max_chunks;
+  Join j;
+  j.add(a, at, chunks, alone ? 0 : wave * Join::SETS, alone ? Join::SETS : 4 * Join::SETS, lane);
+  if (!alone) {
+    if (lane < Join::LANES) *reinterpret_cast<f32x4*>(&lds[wave][4 * lane]) = j.y;
+    if (lane == 0) lds[wave][D] = j.total;
+    __syncthreads();
+    if (wave > 0) return;
+    j.y = f32x4{}; j.total = 0.f;
+    for (int w = 0; w < 4; ++w) {
+      j.total += lds[w][D];
+      if (lane < Join::LANES) j.y += *reinterpret_cast<const f32x4*>(&lds[w][4 * lane]);
+    }
   }
-  __syncthreads();
-  if ((int)threadIdx.x >= D) return;
-  total = ml_lds[0] + ml_lds[1] + ml_lds[2] + ml_lds[3];
-  const float x = o_lds[0][threadIdx.x] + o_lds[1][threadIdx.x] + o_lds[2][threadIdx.x] + o_lds[3][threadIdx.x];
-  const int G = a.heads / a.cache.kv_heads, head = kvh * G + col % G;
+  const int head = kvh * G + col % G;
   const int64_t row = (int64_t)b * a.tokens + col / G;
-  static_cast<Out*>(a.out)[row * a.out_row + head * D + threadIdx.x] = (Out)(total == 0.f ? 0.f : x / total);
-  if (a.lse && threadIdx.x == 0) a.lse[row * a.heads + head] = (top + __builtin_amdgcn_logf(total)) * LN2;
+  Out* out = static_cast<Out*>(a.out) + row * a.out_row + head * D + lane * 4;
+  if (lane < Join::LANES) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) out[e] = (Out)(j.total == 0.f ? 0.f : j.y[e] / j.total);
+  }
+  if (a.lse && lane == 0) a.lse[row * a.heads + head] = (j.top + __builtin_amdgcn_logf(j.total)) * LN2;
 }
 
 }  // namespace tsdp

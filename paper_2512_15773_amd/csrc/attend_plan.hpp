@@ -2,6 +2,7 @@
 // where a token lies in the pages, how a length is split into chunks.  Plain C++: the CPU tests compile this file alone.
 #pragma once
 #include <stdint.h>
+#include <initializer_list>
 
 #ifdef __HIPCC__
 #define TSDP_HD __host__ __device__ __forceinline__
@@ -52,8 +53,9 @@ TSDP_HD int seen(int i, int nq, int nk, bool causal) {
 // Chunk of a sequence that one workgroup of the paged kernel takes, from the sequence's own length and the columns
 // (queries x heads of a group) alone, so that a result does not depend on the batch around it.
 TSDP_HD int chunk_shift(int len, int cols) {
-  int s = cols <= 16 ? 8 : cols <= 32 ? 9 : cols <= 64 ? 10 : 11;
+  int s = cols <= 16 ? 8 : 10;
   if (len > (1 << 14) && s < 10) s = 10;
+  if (len > (1 << 16) && cols <= 16) s = 11;
   return s;
 }
 TSDP_HD int chunks_of(int len, int cols) {
@@ -63,10 +65,8 @@ TSDP_HD int chunks_of(int len, int cols) {
 // the most chunks that a length of at most max_len has
 inline int most_chunks(int max_len, int cols) {
   int n = chunks_of(max_len, cols);
-  if (max_len > (1 << 14)) {
-    const int below = chunks_of(1 << 14, cols);
-    if (below > n) n = below;
-  }
+  for (int at : {1 << 14, 1 << 16})              // where chunks grow
+    if (max_len > at && chunks_of(at, cols) > n) n = chunks_of(at, cols);
   return n;
 }
 

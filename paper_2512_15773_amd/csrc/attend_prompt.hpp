@@ -383,138 +383,4 @@ __global__ __launch_bounds__(NW * 64, WAVES) void k_prompt_bf16(PromptArgs a) {
   if (a.lse && half == 0 && i < t.nq) a.lse[(int64_t)(t.q_lo + i) * a.heads + t.head] = (w.m + __builtin_amdgcn_logf(l)) * LN2;
 }
 
-// fp32: the same walk with mfma_f32_32x32x2_f32.  A lane's 16-byte chunk of a key feeds four of them (MFMA j contracts dims
-// 8 s + j and 8 s + 4 + j); the score register x feeds the value product at key 8 (x / 4) + 4 half + x % 4.
-template <int D, int NW>
-__global__ __launch_bounds__(NW * 64) void k_prompt_f32(PromptArgs a) {
-  constexpr int KT = 32, CH = D / 4, DT = D / 32, TQ = 32 * NW, TILE = KT * D, ROUNDS = KT * CH / (NW * 64), RPR = NW * 64 / CH;
-  static_assert(ROUNDS >= 1 && KT * CH % (NW * 64) == 0, "a tile is whole rounds of the workgroup's loads");
-  __shared__ __align__(16) float lds[2][2][TILE];
-  __shared__ uint32_t unusual[NW];
-  PromptTile t;
-  if (!prompt_tile<TQ>(a, t)) return;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int col = lane & 31, half = lane >> 5;
-  const int i0 = t.i0 + wave * 32, i = i0 + col;
-  const int mine = i < t.nq ? seen(i, t.nq, t.nk, a.causal) : 0;
-  const int all = i0 >= t.nq ? 0 : seen(i0, t.nq, t.nk, a.causal);
-  const int some = i0 >= t.nq ? 0 : seen(min(i0 + 31, t.nq - 1), t.nq, t.nk, a.causal);
-  const int last = seen(min(t.i0 + TQ, t.nq) - 1, t.nq, t.nk, a.causal);
-  const int first = seen(t.i0, t.nq, t.nk, a.causal);
-  const int tiles = (last + KT - 1) / KT;
-  if (lane == 0) unusual[wave] = 0;
-
-  const float* q = static_cast<const float*>(a.q) + (int64_t)(t.q_lo + min(i, t.nq - 1)) * a.q_row + t.head * D;
-  f32x4 qf[D / 8];
-#pragma unroll
-  for (int s = 0; s < D / 8; ++s) qf[s] = *reinterpret_cast<const f32x4*>(q + 8 * s + 4 * half);
-
-  const float* kb = static_cast<const float*>(a.k) + (int64_t)t.k_lo * a.k_row + t.kv_head * D;
-  const float* vb = static_cast<const float*>(a.v) + (int64_t)t.k_lo * a.v_row + t.kv_head * D;
-  const int sr = wave * (64 / CH) + lane / CH, pc = lane % CH;
-  auto stage = [&](int tile, int buf) {
-#pragma unroll
-    for (int n = 0; n < ROUNDS; ++n) {
-      const int r = n * RPR + sr;
-      const int64_t row = min(tile * KT + r, t.nk - 1);
-      float* at = &lds[buf][0][0] + (n * NW + wave) * 256;
-      to_lds(kb + row * a.k_row + (pc ^ key_swizzle<CH>(r)) * 4, at);
-      to_lds(vb + row * a.v_row + pc * 4, at + TILE);
-    }
-  };
-
-  f32x16 o[DT];
-#pragma unroll
-  for (int d = 0; d < DT; ++d) o[d] = f32x16{};
-  float m = -INFINITY, l = 0.f;
-  if (tiles > 0) stage(0, 0);
-  for (int n = 0; n < tiles; ++n) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    const float* kt = &lds[n & 1][0][0];
-    const float* vt = kt + TILE;
-    if ((n + 1) * KT > first) {
-      bool bad = false;
-#pragma unroll
-      for (int x = 0; x < ROUNDS; ++x) {
-        const f32x4 w = *reinterpret_cast<const f32x4*>(vt + (x * NW + wave) * 256 + lane * 4);
-#pragma unroll
-        for (int y = 0; y < 4; ++y) bad |= not_finite_f32(w[y]);
-      }
-      if (__ballot(bad) && lane == 0) unusual[wave] = 1;
-    }
-    __syncthreads();
-    if (n + 1 < tiles) stage(n + 1, (n + 1) & 1);
-    if (n * KT >= some) continue;
-    f32x16 s = f32x16{};
-#pragma unroll
-    for (int x = 0; x < D / 8; ++x) {
-      const f32x4 k = *reinterpret_cast<const f32x4*>(kt + col * D + (((2 * x + half) ^ key_swizzle<CH>(col)) << 2));
-#pragma unroll
-      for (int j = 0; j < 4; ++j) s = __builtin_amdgcn_mfma_f32_32x32x2f32(k[j], qf[x][j], s, 0, 0, 0);
-    }
-    const bool masked = (n + 1) * KT > all;
-    if (masked) {
-      const int left = mine - n * KT;
-#pragma unroll
-      for (int x = 0; x < 16; ++x)
-        if (8 * (x / 4) + 4 * half + x % 4 >= left) s[x] = -INFINITY;
-    }
-    float top = s[0];
-#pragma unroll
-    for (int x = 1; x < 16; ++x) top = fmaxf(top, s[x]);
-    top = max_halves(top) * a.c;
-    if (__any(top > m + 8.f)) {
-      const float to = top > m + 8.f ? top : m, f = to == m ? 1.f : __builtin_amdgcn_exp2f(m - to);   // each query by its own scores
-      m = to;
-      l *= f;
-#pragma unroll
-      for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int x = 0; x < 16; ++x) o[d][x] *= f;
-    }
-    const float sub = m == -INFINITY ? 0.f : m;
-#pragma unroll
-    for (int x = 0; x < 16; ++x) {
-      s[x] = __builtin_amdgcn_exp2f(fmaf(s[x], a.c, -sub));
-      l += s[x];
-    }
-    if (masked && any_of<NW>(unusual)) {
-#pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        f32x16 marks = f32x16{};
-#pragma unroll
-        for (int x = 0; x < 16; ++x) {
-          const int key = 8 * (x / 4) + 4 * half + x % 4;
-          const float v = vt[key * D + 32 * d + col];
-          const bool bad = not_finite_f32(v);
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(bad ? 0.f : v, s[x], o[d], 0, 0, 0);
-          marks = __builtin_amdgcn_mfma_f32_32x32x2f32(bad ? 1.f : 0.f, n * KT + key < mine ? 1.f : 0.f, marks, 0, 0, 0);
-        }
-#pragma unroll
-        for (int x = 0; x < 16; ++x)
-          if (marks[x] != 0.f) o[d][x] = NAN;
-      }
-    } else {
-#pragma unroll
-      for (int x = 0; x < 16; ++x)
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(vt[(8 * (x / 4) + 4 * half + x % 4) * D + 32 * d + col], s[x], o[d], 0, 0, 0);
-    }
-  }
-  l = sum_halves(l);
-  if (i >= t.nq) return;
-  float* out = static_cast<float*>(a.out) + (int64_t)(t.q_lo + i) * a.out_row + t.head * D;
-#pragma unroll
-  for (int d = 0; d < DT; ++d)
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      f32x4 y;
-#pragma unroll
-      for (int z = 0; z < 4; ++z) y[z] = l == 0.f ? 0.f : o[d][4 * x + z] / l;
-      *reinterpret_cast<f32x4*>(out + 32 * d + 8 * x + 4 * half) = y;
-    }
-  if (a.lse && half == 0) a.lse[(int64_t)(t.q_lo + i) * a.heads + t.head] = (m + __builtin_amdgcn_logf(l)) * LN2;
-}
-
 }  // namespace tsdp
