@@ -77,7 +77,7 @@ template <int D>
 void launch_prompt(int type, PromptArgs a, hipStream_t s) {
   if (type == 0) {
     const dim3 grid = prompt_grid<64>(a);
-    hipLaunchKernelGGL((k_wide<D, HELD_F32, true, 3, float, false, PromptArgs>), grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((k_wide<D, HELD_F32, true, 3, float, false, PromptArgs>), grid, dim3(256 * WIDE_GROUPS<false>), 0, s, a);
     return;
   }
   // Sequences of at most 320 keys on average: three waves a SIMD instead of the overlapped loop (256 of 96 tokens, 8 heads of
@@ -99,7 +99,7 @@ void launch_paged(const PagedArgs& a, hipStream_t s) {
   if (a.cols <= 16)
     hipLaunchKernelGGL((k_paged<D, HELD, QF32, NP, Out>), dim3((unsigned)bk, a.max_chunks), dim3(256), 0, s, a);
   else
-    hipLaunchKernelGGL((k_wide<D, HELD, QF32, NP, Out, true, PagedArgs>), dim3((unsigned)(bk * ((a.cols + 63) / 64)), a.max_chunks), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((k_wide<D, HELD, QF32, NP, Out, true, PagedArgs>), dim3((unsigned)(bk * ((a.cols + 63) / 64)), a.max_chunks), dim3(256 * WIDE_GROUPS<true>), 0, s, a);
   if (a.max_chunks <= 1) return;
   if (a.max_chunks <= JOIN_ONE)
     hipLaunchKernelGGL((k_paged_join<D, Out, 4>), dim3((unsigned)((int64_t)a.B * a.cache.kv_heads * ((a.cols + 3) / 4))), dim3(256), 0, s, a);
