@@ -256,8 +256,6 @@ __global__ __launch_bounds__(NW * 64, WAVES) void k_prompt_bf16(PromptArgs a) {
     float f;
     __builtin_amdgcn_s_waitcnt(VM_NONE);
     __syncthreads();
-    s[0] = w.scores(k0, 0, lane);
-    w.maximum(s[0], a.c, f);
     // first and second half of a tile: K, V its buffers, KN the next tile's keys, VL the last one's values
 #define TSDP_FIRST(FIRST, K, VL) w.template half_tile<FIRST, false, !(FIRST), false>(ring, s[1], s[0], p[0], p[1], a.c, K, 32, VL, 32, lane)
 #define TSDP_SECOND(LAST, KN, V) w.template half_tile<false, LAST, false, !(LAST)>(ring, s[0], s[1], p[1], p[0], a.c, KN, 0, V, 0, lane)
@@ -269,6 +267,14 @@ __global__ __launch_bounds__(NW * 64, WAVES) void k_prompt_bf16(PromptArgs a) {
     TSDP_KEYS((N) + 2, K);                                                                                        \
     TSDP_VALUES((N) + 1, VN);                                                                                     \
   } while (0)
+    if (some == 0) {                         // a wave behind the last query only loads
+      for (int n = 0; n < full; n += 2) {
+        TSDP_MIDDLE(n, k0, v1);
+        if (n + 1 < full) TSDP_MIDDLE(n + 1, k1, v0);
+      }
+    } else {
+    s[0] = w.scores(k0, 0, lane);
+    w.maximum(s[0], a.c, f);
     TSDP_FIRST(true, k0, v1);
     TSDP_MIDDLE(0, k0, v1);
     int n = 0;
@@ -288,6 +294,7 @@ __global__ __launch_bounds__(NW * 64, WAVES) void k_prompt_bf16(PromptArgs a) {
     } else {
       TSDP_SECOND(true, k1, v0);
       w.product(p[1], v0, 32, lane);
+    }
     }
 #undef TSDP_FIRST
 #undef TSDP_SECOND
