@@ -369,8 +369,7 @@ class Tsdp:
     def tsdp_cache_read(self, cache, row_ptr, start, rows, dtype, out=None, stream=None):
         """Positions start[b] .. of every environment as packed rows (k, v); out: such a pair to write into."""
         if out is None:
-            both = torch.empty((2, rows, cache.kv_heads, cache.head_dim), dtype=dtype, device=row_ptr.device)
-            out = both[0], both[1]
+            out = row_ptr.new_empty((2, rows, cache.kv_heads, cache.head_dim), dtype=dtype).unbind()
         assert out[0].dtype is dtype and out[0].shape[0] == rows, "out must hold `rows` rows of the given type"
         self._cache_rows(self.lib.tsdp_cache_read, cache, row_ptr, start, out[0], out[1], stream)
         return out

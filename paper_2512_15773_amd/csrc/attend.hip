@@ -35,7 +35,8 @@ CacheView view_of(const tsdp_kv_cache* k) {
 
 template <template <typename, int, int> class Kernel, int HELD, int D>
 void launch_cache(int type, const CacheRows& a, hipStream_t s) {
-  const dim3 grid((a.R_cap + 3) / 4);
+  const int64_t rows = 4 * (int64_t)a.per_wave;
+  const dim3 grid((unsigned)((a.R_cap + rows - 1) / rows));
   if (type == 0) hipLaunchKernelGGL((Kernel<float, HELD, D>::fn), grid, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((Kernel<__bf16, HELD, D>::fn), grid, dim3(256), 0, s, a);
 }
@@ -60,6 +61,7 @@ int cache_rows(tsdp_ctx* c, const tsdp_kv_cache* cache, int B, int R_cap, int ty
   a.c = view_of(cache);
   a.B = B; a.R_cap = R_cap; a.row_ptr = row_ptr; a.start = start;
   a.k = k; a.v = v; a.k_row = k_row; a.v_row = v_row; a.status = ctx_status(c);
+  a.per_wave = std::max(1, 64 / (2 * cache->kv_heads * (cache->head_dim / 8)));
   const hipStream_t s = (hipStream_t)stream;
   if (cache->head_dim == 32) launch_cache_held<Kernel, 32>(cache->type, type, a, s);
   else if (cache->head_dim == 64) launch_cache_held<Kernel, 64>(cache->type, type, a, s);

@@ -1,7 +1,7 @@
 // The paged key / value cache: rows of new tokens written into its pages (quantised on the way) and read back.
 //
-// Both kernels are one pass over the data, bound by HBM: a wave takes one token's row of keys and values, finds the
-// environment that the row belongs to and the page of its position, and moves 8 elements a lane and step.
+// Both kernels are one pass over the data, bound by HBM: a wave takes one token's row of keys and values (several, where they
+// are short), finds the environment that the row belongs to and the page of its position, and moves 8 elements a lane and step.
 //
 // 8 bits (gfx950 converts to and from them in one instruction): blocks of 32 elements along a head share one power of two,
 // the smallest 2^e with max|x| <= 448 * 2^e, and are held as e4m3 of x * 2^-e, rounded to the nearest, ties to even.  The
@@ -19,18 +19,30 @@ struct CacheRows {
   const int32_t* row_ptr; const int32_t* start;
   void* k; void* v;                          // packed rows
   int64_t k_row, v_row;                      // elements from one row to the next
+  int per_wave;                              // rows a wave takes: as many as 64 lanes of 8 elements hold, one at least
   int32_t* status;
 };
 
-// Page and place of packed row r; page -1: outside.  r is uniform in the wave; false: no live row.
-__device__ __forceinline__ bool place_of(const CacheRows& a, int r, int& page, int& token) {
-  const int b = count_upto(a.B, r, [&](int i) { return a.row_ptr[i]; });
+// A lane's row, first unit of 8 elements, page and place; page -1: outside.  False: no live row.
+__device__ __forceinline__ bool place_of(const CacheRows& a, int units, int lane, int& r, int& u, int& page, int& token) {
+  const int first = __builtin_amdgcn_readfirstlane((blockIdx.x * 4 + (threadIdx.x >> 6)) * a.per_wave);
+  if (first >= a.R_cap) return false;
+  if (first == 0 && lane == 0 && a.row_ptr[a.B] > a.R_cap) report(a.status, STATUS_ROWS);
+  int b = count_upto(a.B, first, [&](int i) { return a.row_ptr[i]; });
+  r = first; u = lane;
+  if (a.per_wave > 1) {
+    const int n = lane / units;
+    if (n >= a.per_wave || first + n >= a.R_cap) return false;
+    r += n; u -= n * units;
+    while (b < a.B && a.row_ptr[b + 1] <= r) ++b;
+  }
   if (b >= a.B) return false;
-  const int first = a.row_ptr[b];
-  if (r < first) return false;
-  const long pos = (long)a.start[b] + (r - first);
+  const int start = a.row_ptr[b];
+  if (r < start) return false;
+  const long pos = (long)a.start[b] + (r - start);
   page = pos < 0 ? -1 : page_of(a.c, b, pos >> a.c.page_shift);
   token = (int)(pos & ((1L << a.c.page_shift) - 1));
+  if (page < 0 && u == 0) report(a.status, STATUS_PAGE);
   return true;
 }
 
@@ -70,18 +82,10 @@ __device__ __forceinline__ float quad_max(float x) {
 
 template <typename In, int HELD, int D>
 __global__ __launch_bounds__(256) void k_cache_write(CacheRows a) {
-  const int r = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
-  if (r >= a.R_cap) return;
-  const int lane = threadIdx.x & 63;
-  if (r == 0 && lane == 0 && a.row_ptr[a.B] > a.R_cap) report(a.status, STATUS_ROWS);
-  int page, token;
-  if (!place_of(a, r, page, token)) return;
-  if (page < 0) {
-    if (lane == 0) report(a.status, STATUS_PAGE);
-    return;
-  }
-  const int units = a.c.kv_heads * (D / 8);
-  for (int u = lane; u < 2 * units; u += 64) {
+  const int lane = threadIdx.x & 63, units = a.c.kv_heads * (D / 8);
+  int r, u, page, token;
+  if (!place_of(a, 2 * units, lane, r, u, page, token) || page < 0) return;
+  for (; u < 2 * units; u += 64) {
     const bool val = u >= units;
     const int e = (val ? u - units : u) * 8, head = e / D, off = e % D;
     const In* src = val ? static_cast<const In*>(a.v) + r * a.v_row : static_cast<const In*>(a.k) + r * a.k_row;
@@ -117,15 +121,10 @@ __global__ __launch_bounds__(256) void k_cache_write(CacheRows a) {
 // A position outside the pages reads as zeros.
 template <typename Out, int HELD, int D>
 __global__ __launch_bounds__(256) void k_cache_read(CacheRows a) {
-  const int r = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
-  if (r >= a.R_cap) return;
-  const int lane = threadIdx.x & 63;
-  if (r == 0 && lane == 0 && a.row_ptr[a.B] > a.R_cap) report(a.status, STATUS_ROWS);
-  int page, token;
-  if (!place_of(a, r, page, token)) return;
-  if (page < 0 && lane == 0) report(a.status, STATUS_PAGE);
-  const int units = a.c.kv_heads * (D / 8);
-  for (int u = lane; u < 2 * units; u += 64) {
+  const int lane = threadIdx.x & 63, units = a.c.kv_heads * (D / 8);
+  int r, u, page, token;
+  if (!place_of(a, 2 * units, lane, r, u, page, token)) return;
+  for (; u < 2 * units; u += 64) {
     const bool val = u >= units;
     const int e = (val ? u - units : u) * 8, head = e / D, off = e % D;
     Out* dst = val ? static_cast<Out*>(a.v) + r * a.v_row : static_cast<Out*>(a.k) + r * a.k_row;
