@@ -94,14 +94,14 @@ def test_keys_that_a_query_sees(plan):
 def test_chunks_cover_a_length_and_their_bound_holds(plan):
     rng = np.random.default_rng(0)
     for cols in (1, 8, 16, 17, 33, 64, 65, 1024):
-        lens = [0, 1, 255, 256, 257, 16383, 16384, 16385, 65536, 65537, 131072] + rng.integers(0, 300000, 50).tolist()
+        lens = [0, 1, 255, 256, 257, 1024, 1025, 16383, 16384, 16385, 65536, 65537, 131072] + rng.integers(0, 300000, 50).tolist()
         for n in lens:
             c = plan.chunk(n, cols)
             assert c >= 128 and c % 128 == 0                          # four waves of whole tiles
             assert plan.chunks(n, cols) == -(-n // c)
         for most in lens:
             bound = plan.most(most, cols)
-            for n in [x for x in lens if x <= most] + [min(most, 16384), min(most, 65536)]:
+            for n in [x for x in lens if x <= most] + [min(most, 1024), min(most, 16384), min(most, 65536)]:
                 assert plan.chunks(n, cols) <= bound, (n, most, cols)
 
 
