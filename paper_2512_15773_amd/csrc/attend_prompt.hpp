@@ -65,7 +65,12 @@ __device__ __forceinline__ void to_lds(const void* g, void* lds) {
 template <int CH> __device__ __forceinline__ int key_swizzle(int row) { return CH >= 16 ? row & 15 : CH == 8 ? (row >> 1) & 7 : (row >> 2) & 3; }
 template <int CH> __device__ __forceinline__ int value_swizzle(int row) { return CH >= 16 ? (row & 3) << 2 : CH == 8 ? ((row >> 1) & 1) << 2 : 0; }
 
-constexpr int VM_NONE = 0x0F70;              // s_waitcnt vmcnt(0)
+// Until all of this wave's loads into LDS have landed.  (The builtin: the compiler counts with it.)
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0F70);        // vmcnt(0)
+  asm volatile("" ::: "memory");
+}
 
 // bf16.  A wave owns 32 queries.  Keys go by 32 (half a tile) through three stages that do not depend on each other and are
 // issued into each other: scores of the next 32 keys (matrix pipe), softmax of these (vector pipe), product of the last 32
@@ -254,7 +259,7 @@ __global__ __launch_bounds__(NW * 64, WAVES) void k_prompt_bf16(PromptArgs a) {
     f32x16 s[2];
     bf16x8 p[2][2], ring[C::RING];
     float f;
-    __builtin_amdgcn_s_waitcnt(VM_NONE);
+    wait_loads();
     __syncthreads();
     // first and second half of a tile: K, V its buffers, KN the next tile's keys, VL the last one's values
 #define TSDP_FIRST(FIRST, K, VL) w.template half_tile<FIRST, false, !(FIRST), false>(ring, s[1], s[0], p[0], p[1], a.c, K, 32, VL, 32, lane)
@@ -262,7 +267,7 @@ __global__ __launch_bounds__(NW * 64, WAVES) void k_prompt_bf16(PromptArgs a) {
     // between them, in tile N with keys in K and the other buffer of values VN
 #define TSDP_MIDDLE(N, K, VN)                                                                                     \
   do {                                                                                                            \
-    __builtin_amdgcn_s_waitcnt(VM_NONE);                                                                          \
+    wait_loads();                                                                          \
     __syncthreads();                                                                                              \
     TSDP_KEYS((N) + 2, K);                                                                                        \
     TSDP_VALUES((N) + 1, VN);                                                                                     \
@@ -304,7 +309,7 @@ __global__ __launch_bounds__(NW * 64, WAVES) void k_prompt_bf16(PromptArgs a) {
     from = full;
     if (any_of<NW>(rises)) {                 // once more from the start
       from = 0;
-      __builtin_amdgcn_s_waitcnt(VM_NONE);
+      wait_loads();
       __syncthreads();                       // nobody's loads land behind the new ones
       TSDP_KEYS(0, k0);
       TSDP_KEYS(1, k1);
@@ -316,7 +321,7 @@ __global__ __launch_bounds__(NW * 64, WAVES) void k_prompt_bf16(PromptArgs a) {
 #pragma unroll
   for (int d = 0; d < C::DT; ++d) gone[d] = 0;
   auto plain = [&](int n, uint8_t* k, uint8_t* kn, uint8_t* v, uint8_t* vn) __attribute__((always_inline)) {
-    __builtin_amdgcn_s_waitcnt(VM_NONE);
+    wait_loads();
     bool bad = false;
 #pragma unroll
     for (int x = 0; x < C::ROUNDS; ++x) {
