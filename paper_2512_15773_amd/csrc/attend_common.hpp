@@ -88,8 +88,8 @@ __device__ __forceinline__ bool not_finite_f32(float f) { return (as_u32(f) & 0x
 // own scores): weights up to 2^48 lose nothing in floating types, and leave 2^59 to the values before a sum of 2^20 of them
 // overflows.
 constexpr float MOST_RISE = 48.f;
-// what a sum of weights exceeds if one of them rose further (or was infinite), or if the first keys gave no maximum at all
-__device__ __forceinline__ float most_sum(float m) { return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(MOST_RISE); }
+// what a sum of weights exceeds if one of them rose further (or was infinite); any does if the first keys gave no maximum at all
+__device__ __forceinline__ float most_sum(float m) { return m == -INFINITY ? -1.f : __builtin_amdgcn_exp2f(MOST_RISE); }
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 }  // namespace tsdp

@@ -267,7 +267,7 @@ __global__ __launch_bounds__(NW * 64, WAVES) void k_prompt_bf16(PromptArgs a) {
     // between them, in tile N with keys in K and the other buffer of values VN
 #define TSDP_MIDDLE(N, K, VN)                                                                                     \
   do {                                                                                                            \
-    wait_loads();                                                                          \
+    wait_loads();                                                                                                 \
     __syncthreads();                                                                                              \
     TSDP_KEYS((N) + 2, K);                                                                                        \
     TSDP_VALUES((N) + 1, VN);                                                                                     \
@@ -304,7 +304,7 @@ __global__ __launch_bounds__(NW * 64, WAVES) void k_prompt_bf16(PromptArgs a) {
 #undef TSDP_FIRST
 #undef TSDP_SECOND
 #undef TSDP_MIDDLE
-    if (__any(w.l > most_sum(w.m)) && lane == 0) rises[wave] = 1;
+    if (some > 0 && __any(w.l > most_sum(w.m)) && lane == 0) rises[wave] = 1;
     __syncthreads();
     from = full;
     if (any_of<NW>(rises)) {                 // once more from the start

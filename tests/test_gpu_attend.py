@@ -417,6 +417,170 @@ def test_paged_lengths_beyond_their_bound_are_clipped_and_reported(ctx):
     check(got[2:], None, ao.attend(f64(q[2:]), values[0][2], values[1][2], 32 ** -0.5, True), 32, 64, "bf16", WEIGHTS["paged"]["bf16"], "table")
 
 
+# ---- what the above leaves open: many columns over several chunks, maxima that move, hidden memory, extremes
+
+def put(c, which, b, rows):
+    """rows [n, kv, dim] (float64) to positions 0 .. of environment b, as the cache holds them; returns the held values."""
+    import torch
+    page, n = c.k.shape[2], rows.shape[0]
+    x, s = ((c.k, c.k_scale), (c.v, c.v_scale))[which]
+    table = c.page_table.cpu().numpy()
+    at = (torch.from_numpy(table[b, np.arange(n) // page]).long().cuda(), torch.from_numpy(np.arange(n) % page).cuda())
+    if s is None:
+        y = torch.from_numpy(rows.astype(np.float32)).to(x.dtype)
+        x[at[0], :, at[1]] = y.cuda()
+        return y.double().numpy()
+    codes, scale = ao.mx8(rows)
+    x[at[0], :, at[1]] = torch.from_numpy(codes).cuda()
+    s[at[0], :, at[1]] = torch.from_numpy(scale).cuda()
+    return ao.mx8_values(codes, scale)
+
+
+KINDS = (("fp32", "fp32", "fp32"), ("bf16", "bf16", "bf16"), ("bf16", "bf16", "fp32"), ("fp32", "mx8", "fp32"), ("bf16", "mx8", "bf16"), ("bf16", "mx8", "fp32"))
+
+
+@pytest.mark.parametrize("dtype,held,out", KINDS)
+@pytest.mark.parametrize("dim,heads,kv,tokens,page", ((32, 6, 2, 9, 16), (64, 4, 1, 33, 64), (128, 8, 4, 9, 128)))
+@pytest.mark.parametrize("causal", (True, False))
+def test_paged_many_columns(ctx, dtype, held, out, dim, heads, kv, tokens, page, causal):
+    """18, 27 and 132 columns of a kv head, over lengths of none to several chunks."""
+    import torch
+    rng = np.random.default_rng(dim * 3 + tokens)
+    lens = [0, 1, tokens - 1, tokens + 1, 31, 32, 33, 130, 1023, 1024, 1025, 2100]
+    c, values = filled(rng, held, lens, kv, page, dim, 1.3)
+    B = len(lens)
+    q = draw(rng, (B * tokens, heads, dim), dtype, 1.3)
+    lse = torch.full((B * tokens, heads), 7.0, device="cuda")
+    got = ctx.tsdp_attend_paged(q, c, i32(lens), max(lens), tokens=tokens, causal=causal, scale=0.13, out_dtype=torch_dtype(out), lse=lse)
+    for b, n in enumerate(lens):
+        r = slice(b * tokens, (b + 1) * tokens)
+        check(got[r], lse[r], ao.attend(f64(q[r]), values[0][b], values[1][b], 0.13, causal), dim, n, out, WEIGHTS["paged"][out], (b, n))
+    from paper_2512_15773_amd import KvCache
+    for b in (3, 9, 11):                                     # alone, and with another bound of the lengths
+        one, r = KvCache(c.k, c.v, c.page_table[b:b + 1], c.k_scale, c.v_scale), slice(b * tokens, (b + 1) * tokens)
+        for most in (lens[b], 40000):
+            again = ctx.tsdp_attend_paged(q[r], one, i32([lens[b]]), most, tokens=tokens, causal=causal, scale=0.13, out_dtype=torch_dtype(out))
+            assert torch.equal(again, got[r]), (b, most)
+    assert ctx.tsdp_status() == 0
+
+
+@pytest.mark.parametrize("dtype,held,out", KINDS)
+@pytest.mark.parametrize("dim", (32, 64, 128))
+@pytest.mark.parametrize("tokens", (1, 9))
+@pytest.mark.parametrize("n", (300, 1400))
+def test_paged_over_large_scores_and_far_maxima(ctx, dtype, held, out, dim, tokens, n):
+    """Scores of some hundreds that grow and fall along the keys: maxima move often for one head and never for the other."""
+    rng = np.random.default_rng(n + dim)
+    k = rng.standard_normal((n, 1, dim)) * 0.2
+    k[:, 0, 0] = np.concatenate([np.linspace(-30, 30, n // 2), np.linspace(30, -30, n - n // 2)])
+    q = rng.standard_normal((tokens, 2, dim)) * 0.2
+    q[:, 0, 0], q[:, 1, 0] = 10.0, -10.0
+    c = new_cache(rng, held, 1, -(-n // 64), 1, 64, dim)
+    import torch
+    k, v = put(c, 0, 0, k), put(c, 1, 0, rng.standard_normal((n, 1, dim)))
+    q = torch.from_numpy(q.astype(np.float32)).to(torch_dtype(dtype)).cuda()
+    for causal in (True, False):
+        lse = torch.zeros(tokens, 2, device="cuda")
+        got = ctx.tsdp_attend_paged(q, c, i32([n]), n, tokens=tokens, causal=causal, scale=1.0, out_dtype=torch_dtype(out), lse=lse)
+        check(got, lse, ao.attend(f64(q), k, v, 1.0, causal), dim, n, out, WEIGHTS["paged"][out], causal)
+
+
+LOST = 70                                                    # first keys whose scores are all -infinity
+
+
+def lost_keys(rng, n, dim):
+    """Queries and keys: the first scores overflow to -infinity, the others are near -300 (a power of two that fp32 does not hold)."""
+    k = rng.standard_normal((n, 1, dim)) * 0.3
+    k[:LOST, 0, 0], k[LOST:, 0, 0], k[:, 0, 1] = -1e20, 0.0, -300.0
+    q = rng.standard_normal((n, 2, dim)) * 0.3
+    q[:, :, 0], q[:, :, 1] = 1e20, 1.0
+    return q, k
+
+
+@pytest.mark.parametrize("dtype", ("fp32", "bf16"))
+@pytest.mark.parametrize("n,dim", ((200, 32), (200, 64), (500, 64), (300, 128)))
+def test_prompt_whose_first_scores_overflow(ctx, dtype, n, dim):
+    """Weights of zero: the result is that of the other keys."""
+    import torch
+    rng = np.random.default_rng(n + dim)
+    to = lambda x: torch.from_numpy(x.astype(np.float32)).to(torch_dtype(dtype)).cuda()
+    q, k = (to(x) for x in lost_keys(rng, n, dim))
+    v, lse = draw(rng, (n, 1, dim), dtype), torch.zeros(n, 2, device="cuda")
+    got = ctx.tsdp_attend_prompt(q, k, v, i32([0, n]), causal=False, scale=1.0, lse=lse)
+    check(got, lse, ao.attend(f64(q), f64(k)[LOST:], f64(v)[LOST:], 1.0, False), dim, n, dtype, WEIGHTS["prompt"][dtype], n)
+
+
+@pytest.mark.parametrize("dtype,held,out", KINDS)
+@pytest.mark.parametrize("dim", (32, 64, 128))
+@pytest.mark.parametrize("tokens,n", ((1, 300), (1, 1400), (9, 300), (9, 1400)))
+def test_paged_whose_first_scores_overflow(ctx, dtype, held, out, dim, tokens, n):
+    import torch
+    rng = np.random.default_rng(n + dim + tokens)
+    q, k = lost_keys(rng, n, dim)
+    if held == "mx8":                                        # next to 1e20 a block holds nothing else, -300 is lost there: no key but
+        k[:LOST, 0, 2:] = 0.0                                # the first ones has to be exact
+    c = new_cache(rng, held, 1, -(-n // 64), 1, 64, dim)
+    k, v = put(c, 0, 0, k), put(c, 1, 0, rng.standard_normal((n, 1, dim)))
+    q, lse = torch.from_numpy(q[:tokens].astype(np.float32)).to(torch_dtype(dtype)).cuda(), torch.zeros(tokens, 2, device="cuda")
+    got = ctx.tsdp_attend_paged(q, c, i32([n]), n, tokens=tokens, causal=False, scale=1.0, out_dtype=torch_dtype(out), lse=lse)
+    check(got, lse, ao.attend(f64(q), k[LOST:], v[LOST:], 1.0, False), dim, n, out, WEIGHTS["paged"][out], n)
+
+
+@pytest.mark.parametrize("dtype,held", (("fp32", "fp32"), ("bf16", "bf16"), ("bf16", "mx8"), ("fp32", "mx8")))
+@pytest.mark.parametrize("dim", (32, 64, 128))
+def test_paged_many_columns_hide_what_is_masked(ctx, dtype, held, dim):
+    """As for few columns: a value that is not finite reaches the tokens from its own on, at its own element; a page outside the
+    pool is not attended to."""
+    import torch
+    rng = np.random.default_rng(dim)
+    n, tokens, heads, own = 1024 + 301, 12, 4, 5             # the value is that of the sixth of twelve new tokens
+    c, values = filled(rng, held, [n], 2, 64, dim)
+    q = draw(rng, (tokens, heads, dim), dtype)
+    run = lambda: ctx.tsdp_attend_paged(q, c, i32([n]), n, tokens=tokens)
+    clean, pos = run(), n - tokens + own
+    page, t = int(c.page_table[0, pos // 64]), pos % 64
+    for e in (0, 13, dim - 1):
+        old = c.v[page, 1, t, e].clone()
+        c.v[page, 1, t, e] = 127 if held == "mx8" else float("inf")
+        got = run()
+        c.v[page, 1, t, e] = old
+        rest = [i for i in range(dim) if i != e]
+        assert torch.equal(got[:own], clean[:own]) and torch.equal(got[:, :2], clean[:, :2])
+        assert not np.isfinite(f64(got[own:, 2:, e])).any() and torch.equal(got[own:, 2:][..., rest], clean[own:, 2:][..., rest])
+    for column in (1, 17, 20):
+        old = c.page_table[0, column].clone()
+        c.page_table[0, column] = c.k.shape[0] + 5
+        got = run()
+        c.page_table[0, column] = old
+        assert ctx.tsdp_status() == 64
+        keep = np.array([i for i in range(n) if i // 64 != column])
+        for token in (0, own, tokens - 1):
+            see = keep[keep < n - tokens + 1 + token]
+            check(got[token:token + 1], None, ao.attend(f64(q[token:token + 1]), values[0][0][see], values[1][0][see], dim ** -0.5, False),
+                  dim, n, dtype, WEIGHTS["paged"][dtype], (column, token))
+
+
+@pytest.mark.parametrize("where", ("prompt", "few", "many"))
+@pytest.mark.parametrize("dim", (32, 64, 128))
+def test_values_next_to_the_largest(ctx, where, dim):
+    """fp32 values of +-3.4e38 at equal weights of a fourth: nothing overflows on the way to a bf16 part."""
+    import torch
+    rng = np.random.default_rng(dim)
+    most = float(np.finfo(np.float32).max)
+    n, tokens = 4, 1 if where == "few" else 4
+    k = np.zeros((n, 1, dim)); v = np.zeros((n, 1, dim))
+    v[0], v[2] = most, rng.standard_normal((1, dim))
+    q = torch.zeros(tokens, 8, dim, device="cuda")
+    if where == "prompt":
+        to = lambda x: torch.from_numpy(x.astype(np.float32)).cuda()
+        got = ctx.tsdp_attend_prompt(q, to(k), to(v), i32([0, 4]), causal=False)
+    else:
+        c = new_cache(rng, "fp32", 1, 1, 1, 16, dim)
+        put(c, 0, 0, k); put(c, 1, 0, v)
+        got = ctx.tsdp_attend_paged(q, c, i32([4]), 4, tokens=tokens, causal=False)
+    check(got, None, ao.attend(f64(q), k, v, dim ** -0.5, False), dim, n, "fp32", WEIGHTS["paged"]["fp32"], where)
+
+
 # ---- together
 
 def test_an_episode(ctx):
