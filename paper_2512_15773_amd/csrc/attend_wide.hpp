@@ -95,11 +95,21 @@ template <int D> struct WideRow<D, HELD_MX8> {
     }
   }
   __device__ __forceinline__ uint32_t unusual() {
+    // judged by what they widen to: memory that nobody wrote may hold any scale
+    if (scale == 255) {
+#pragma unroll
+      for (int i = 0; i < E / 4; ++i) x[i] = 0;
+      scale = 127;
+      return (1u << E) - 1;
+    }
     uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-      const uint32_t byte = 255u << (8 * (i % 4));
-      if ((x[i / 4] & byte & 0x7F7F7F7Fu) == (byte & 0x7F7F7F7Fu)) { m |= 1u << i; x[i / 4] &= ~byte; }
+    for (int i = 0; i < E / 4; ++i) {
+      const u32x2 y = mx8_to_bf16(x[i], scale_of(scale));
+      const uint32_t bad = not_finite_halves(y[0]) | not_finite_halves(y[1]) << 2;
+      m |= bad << (4 * i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[i] &= bad >> e & 1 ? ~(255u << (8 * e)) : ~0u;
     }
     return m;
   }

@@ -526,6 +526,33 @@ def test_paged_whose_first_scores_overflow(ctx, dtype, held, out, dim, tokens, n
     check(got, lse, ao.attend(f64(q), k[LOST:], v[LOST:], 1.0, False), dim, n, out, WEIGHTS["paged"][out], n)
 
 
+@pytest.mark.parametrize("dtype,held,out", KINDS)
+@pytest.mark.parametrize("dim", (32, 64, 128))
+@pytest.mark.parametrize("tokens", (2, 12))
+def test_paged_memory_behind_a_length_stays_hidden(ctx, dtype, held, out, dim, tokens):
+    """Whatever the places behind a sequence in its last page hold, the result is bit-equal."""
+    import torch
+    rng = np.random.default_rng(dim + tokens)
+    n = 1024 + 70                                            # ends inside a page, 6 places into a tile
+    c, _ = filled(rng, held, [n], 2, 256, dim)
+    q = draw(rng, (tokens, 4, dim), dtype)
+    run = lambda: ctx.tsdp_attend_paged(q, c, i32([n]), n, tokens=tokens, out_dtype=torch_dtype(out))
+    clean, page = run(), int(c.page_table[0, n // 256])
+    assert torch.isfinite(clean).all()
+    pools = [x[page][:, n % 256:] for x in (c.k, c.v)]
+    if held == "mx8":
+        scales = [x[page][:, n % 256:] for x in (c.k_scale, c.v_scale)]
+        for code, scale in ((0x7E, 255), (0x7E, 254), (0xFE, 248), (0, 255), (0x7F, 0), (0x7E, 246), (1, 255)):
+            for x, s in zip(pools, scales):
+                x.fill_(code); s.fill_(scale)
+            assert torch.equal(run(), clean), (code, scale)
+    else:
+        for bad in (float("inf"), -float("inf"), float("nan"), torch.finfo(pools[0].dtype).max, torch.finfo(pools[0].dtype).min):
+            for x in pools:
+                x.fill_(bad)
+            assert torch.equal(run(), clean), bad
+
+
 @pytest.mark.parametrize("dtype,held", (("fp32", "fp32"), ("bf16", "bf16"), ("bf16", "mx8"), ("fp32", "mx8")))
 @pytest.mark.parametrize("dim", (32, 64, 128))
 def test_paged_many_columns_hide_what_is_masked(ctx, dtype, held, dim):
