@@ -7,6 +7,7 @@ Calls only enqueue work on the given (default: torch's current) stream.  The bin
 handed to a call must stay alive until that stream has run the call -- torch's caching allocator does not know of the
 use and would hand a freed tensor's memory out again (keep a reference, or call Tensor.record_stream yourself).
 """
+import contextlib
 import ctypes as C
 import os
 
@@ -111,6 +112,14 @@ def _ptr(t, dtype=None):
 def _stream(stream):
     # the handle alone: building torch's Stream object takes 3 us
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) if stream is None else stream.cuda_stream
+
+
+_CURRENT = contextlib.nullcontext()
+
+
+def _memory_on(stream):
+    """What is allocated inside belongs to the stream that the call runs on: nothing that another stream still uses."""
+    return _CURRENT if stream is None else torch.cuda.stream(stream)
 
 
 _TYPE = {torch.float32: 0, torch.bfloat16: 1}
@@ -369,7 +378,8 @@ class Tsdp:
     def tsdp_cache_read(self, cache, row_ptr, start, rows, dtype, out=None, stream=None):
         """Positions start[b] .. of every environment as packed rows (k, v); out: such a pair to write into."""
         if out is None:
-            out = row_ptr.new_empty((2, rows, cache.kv_heads, cache.head_dim), dtype=dtype).unbind()
+            with _memory_on(stream):
+                out = row_ptr.new_empty((2, rows, cache.kv_heads, cache.head_dim), dtype=dtype).unbind()
         assert out[0].dtype is dtype and out[0].shape[0] == rows, "out must hold `rows` rows of the given type"
         self._cache_rows(self.lib.tsdp_cache_read, cache, row_ptr, start, out[0], out[1], stream)
         return out
@@ -388,7 +398,8 @@ class Tsdp:
         (rows, heads, dim), (k_rows, kv, _) = q.shape, k.shape
         assert dtype in _TYPE and v.shape[0] == k_rows, "q, k and v must be of one type, float32 or bfloat16, and k and v alike"
         if out is None:
-            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            with _memory_on(stream):
+                out = torch.empty_like(q, memory_format=torch.contiguous_format)
         assert out.shape[0] == rows, "out must be alike q"
         qp, q_row = _rows(q, heads, dim, dtype, dev)
         kp, k_row = _rows(k, kv, dim, dtype, dev)
@@ -420,12 +431,12 @@ class Tsdp:
         assert cache.device == dev, "the cache must be on the current device"
         assert dtype in _TYPE and rows == B * tokens and dim == cache.head_dim, "q must be [B * tokens, q_heads, head_dim], float32 or bfloat16"
         if out is None:
-            out = torch.empty_like(q, dtype=out_dtype, memory_format=torch.contiguous_format)
+            with _memory_on(stream):
+                out = torch.empty_like(q, dtype=out_dtype, memory_format=torch.contiguous_format)
         assert out.dtype in _TYPE and out.shape[0] == rows and out_dtype in (None, out.dtype), "out must be alike q, float32 or bfloat16"
         if scratch is None:
-            scratch = self.alloc_scratch(cache, heads, tokens, max_len, B)
-            if scratch is not None and stream is not None:
-                scratch.record_stream(stream)
+            with _memory_on(stream):
+                scratch = self.alloc_scratch(cache, heads, tokens, max_len, B)
         qp, q_row = _rows(q, heads, dim, dtype, dev)
         op, out_row = _rows(out, heads, dim, out.dtype, dev)
         rc = self.lib.tsdp_attend_paged(self.ctx, TsdpHeads(_TYPE[dtype], heads, cache.kv_heads, dim, 1 if causal else 0, dim ** -0.5 if scale is None else scale),

@@ -608,6 +608,30 @@ def test_values_next_to_the_largest(ctx, where, dim):
     check(got, None, ao.attend(f64(q), k, v, dim ** -0.5, False), dim, n, "fp32", WEIGHTS["paged"]["fp32"], where)
 
 
+def test_memory_of_a_call_on_another_stream_is_that_streams(ctx):
+    """Outputs and scratch that a call allocates for a stream it is given: nothing that the current stream still uses."""
+    import torch
+    rng = np.random.default_rng(20)
+    c, _ = filled(rng, "bf16", [5000], 2, 64, 64)
+    q, length = draw(rng, (1, 8, 64), "bf16"), i32([5000])
+    p = [draw(rng, (700, h, 64), "bf16") for h in (8, 2, 2)]
+    ptr, rows, zero = i32([0, 700]), i32([0, 100]), i32([0])
+    calls = (lambda s: ctx.tsdp_attend_paged(q, c, length, 5000, stream=s), lambda s: ctx.tsdp_attend_prompt(*p, ptr, stream=s),
+             lambda s: ctx.tsdp_cache_read(c, rows, zero, 100, torch.bfloat16, stream=s)[0])
+    want = [f(None) for f in calls]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    allocated = []
+    for f in calls:
+        allocated.append(f(side))
+        mine = [s for s in torch.cuda.memory_snapshot() if s["stream"] == side.cuda_stream]
+        at = allocated[-1].data_ptr()
+        assert any(s["address"] <= at < s["address"] + s["total_size"] for s in mine)
+    torch.cuda.synchronize()
+    for x, y in zip(allocated, want):
+        assert torch.equal(x, y)
+
+
 # ---- together
 
 def test_an_episode(ctx):
