@@ -241,7 +241,8 @@ int tsdp_distill_loss_noalloc(tsdp_ctx* ctx, int R, const int32_t* d_row_t, cons
  * tsdp_verify was outside 0..T-1 (clamped), bit 2 = some running environment had sigma_scale <= 0 or NaN (not
  * corrected: the outputs of that environment are undefined, no memory is touched out of bounds), bit 3 = a row
  * environment index given to tsdp_verify was outside the batch of tsdp_set_cond (clamped), bit 4 = a kernel gave up waiting
- * for another workgroup of its launch (cannot happen; the results are undefined, tsdp_load_weights restores the context). */
+ * for another workgroup of its launch (cannot happen; the results are undefined, tsdp_load_weights restores the context),
+ * bits 5 and 6 = attention and cache calls, see there. */
 int tsdp_status(tsdp_ctx* ctx, void* stream, int32_t* h_status);
 
 /* Measurement aid.  tsdp_kernel_timing(ctx, 1) makes the following calls record a pair of HIP events on the
@@ -267,7 +268,8 @@ const char* tsdp_path_name(const tsdp_ctx* ctx, int which);
  * that cache.  These calls use nothing of the context but its device, its error message and its status word, and no
  * memory but the caller's: the context's device must be current (TSDP_E_STATE otherwise), nothing is allocated, no call
  * synchronises, all can be captured in a HIP graph, and calls on different streams may overlap as long as their outputs and
- * scratch are different memory.
+ * scratch are different memory.  Outputs and scratch must not overlap what a call reads.  A call whose launch would need 2^32
+ * threads or more is refused (TSDP_E_SHAPE).
  *
  * Packed rows: environment b owns rows ptr[b] .. ptr[b+1]-1 of its [rows, heads, head_dim] tensors (heads next to each
  * other; *_row is the distance from one row to the next in elements, so a slice of a wider projection can be passed).  The
@@ -277,9 +279,12 @@ const char* tsdp_path_name(const tsdp_ctx* ctx, int which);
  *
  * Keys that a query sees: with causal = 0 all of its environment's; with causal = 1 those up to its own place, the last
  * query standing at the last key (query i of nq sees keys 0 .. nk - nq + i).  A query that sees no key gets zeros and a
- * log-sum of -infinity.  Keys and values that a query does not see do not reach its result, whatever they hold (NaN,
- * infinities, memory never written); a value it sees that is not finite gives NaN or infinity.  A query's result depends on
- * its own environment's rows alone, bit for bit, not on the batch around it.
+ * log-sum of -infinity, and so does one whose scores are all -infinity.  Keys and values that a query does not see do not
+ * reach its result, whatever they hold (NaN, infinities, memory never written).  Of those it sees, a value that is not finite
+ * makes its own element of the result NaN or infinite, a key of NaN all of them; a key of infinity does so too, or weighs nothing
+ * where its score is -infinity.  Products are summed up before they are divided by the sum of the weights, in fp32 with weights
+ * of up to 2^48: values of more than 2^59 in magnitude may overflow.  A query's result depends on its own environment's rows
+ * alone, bit for bit, not on the batch around it.
  *
  * log-sums (d_lse, optional): log sum_j exp(scale <q_i, k_j>), fp32 [query rows, q_heads].
  *
@@ -296,8 +301,8 @@ typedef struct {
  * position p of environment b lies in page page_table[b, p / page_tokens] at place p mod page_tokens.  Environments may share
  * pages.  type 2 holds 8 bits: blocks of 32 elements along a head share one power of two, the smallest 2^e >= 2^-111 with
  * max|x| <= 448 * 2^e (scale pools [pages, kv_heads, page_tokens, head_dim / 32] hold e + 127), and their elements are
- * e4m3 of x * 2^-e, rounded to the nearest, ties to even; what is not finite is held as NaN.  A cache of bf16 takes fp32 rows
- * rounded to the nearest, ties to even. */
+ * e4m3 of x * 2^-e, rounded to the nearest, ties to even; what is not finite is held as NaN, and what is rounded to 2^128
+ * (magnitudes from 248 * 2^120 on) is read as an infinity.  A cache of bf16 takes fp32 rows rounded to the nearest, ties to even. */
 typedef struct {
   int32_t type;           /* what is held: 0 = fp32, 1 = bf16, 2 = 8 bits */
   int32_t kv_heads, head_dim;

@@ -434,6 +434,7 @@ class Tsdp:
             with _memory_on(stream):
                 out = torch.empty_like(q, dtype=out_dtype, memory_format=torch.contiguous_format)
         assert out.dtype in _TYPE and out.shape[0] == rows and out_dtype in (None, out.dtype), "out must be alike q, float32 or bfloat16"
+        assert scratch is None or scratch.get_device() == dev, "scratch must be on the current device"
         if scratch is None:
             with _memory_on(stream):
                 scratch = self.alloc_scratch(cache, heads, tokens, max_len, B)

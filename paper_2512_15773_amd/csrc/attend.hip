@@ -35,8 +35,7 @@ CacheView view_of(const tsdp_kv_cache* k) {
 
 template <template <typename, int, int> class Kernel, int HELD, int D>
 void launch_cache(int type, const CacheRows& a, hipStream_t s) {
-  const int64_t rows = 4 * (int64_t)a.per_wave;
-  const dim3 grid((unsigned)((a.R_cap + rows - 1) / rows));
+  const dim3 grid((unsigned)cache_blocks(a.R_cap, a.c.kv_heads, D));
   if (type == 0) hipLaunchKernelGGL((Kernel<float, HELD, D>::fn), grid, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((Kernel<__bf16, HELD, D>::fn), grid, dim3(256), 0, s, a);
 }
@@ -61,7 +60,7 @@ int cache_rows(tsdp_ctx* c, const tsdp_kv_cache* cache, int B, int R_cap, int ty
   a.c = view_of(cache);
   a.B = B; a.R_cap = R_cap; a.row_ptr = row_ptr; a.start = start;
   a.k = k; a.v = v; a.k_row = k_row; a.v_row = v_row; a.status = ctx_status(c);
-  a.per_wave = std::max(1, 64 / (2 * cache->kv_heads * (cache->head_dim / 8)));
+  a.per_wave = rows_per_wave(cache->kv_heads, cache->head_dim);
   const hipStream_t s = (hipStream_t)stream;
   if (cache->head_dim == 32) launch_cache_held<Kernel, 32>(cache->type, type, a, s);
   else if (cache->head_dim == 64) launch_cache_held<Kernel, 64>(cache->type, type, a, s);
@@ -71,7 +70,7 @@ int cache_rows(tsdp_ctx* c, const tsdp_kv_cache* cache, int B, int R_cap, int ty
 
 template <int TQ>
 dim3 prompt_grid(PromptArgs& a) {
-  a.slots = a.q_cap / TQ + a.B;
+  a.slots = (int)prompt_slots(a.q_cap, a.B, TQ);
   return dim3((unsigned)((int64_t)a.slots * a.heads));
 }
 
@@ -99,14 +98,13 @@ template <int D, int HELD, bool QF32, int NP, typename Out>
 void launch_paged(const PagedArgs& a, hipStream_t s) {
   const int64_t bk = (int64_t)a.B * a.cache.kv_heads;
   if (a.cols <= 16)
-    hipLaunchKernelGGL((k_paged<D, HELD, QF32, NP, Out>), dim3((unsigned)bk, a.max_chunks), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((k_paged<D, HELD, QF32, NP, Out>), dim3((unsigned)paged_blocks(bk, a.cols), a.max_chunks), dim3(256), 0, s, a);
   else
-    hipLaunchKernelGGL((k_wide<D, HELD, QF32, NP, Out, true, PagedArgs>), dim3((unsigned)(bk * ((a.cols + 63) / 64)), a.max_chunks), dim3(256 * WIDE_GROUPS<true>), 0, s, a);
+    hipLaunchKernelGGL((k_wide<D, HELD, QF32, NP, Out, true, PagedArgs>), dim3((unsigned)paged_blocks(bk, a.cols), a.max_chunks), dim3(256 * WIDE_GROUPS<true>), 0, s, a);
   if (a.max_chunks <= 1) return;
-  if (a.max_chunks <= JOIN_ONE)
-    hipLaunchKernelGGL((k_paged_join<D, Out, 4>), dim3((unsigned)((int64_t)a.B * a.cache.kv_heads * ((a.cols + 3) / 4))), dim3(256), 0, s, a);
-  else
-    hipLaunchKernelGGL((k_paged_join<D, Out, 1>), dim3((unsigned)((int64_t)a.B * a.cache.kv_heads * a.cols)), dim3(256), 0, s, a);
+  const dim3 join((unsigned)join_blocks(bk, a.cols, a.max_chunks));
+  if (a.max_chunks <= JOIN_ONE) hipLaunchKernelGGL((k_paged_join<D, Out, 4>), join, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((k_paged_join<D, Out, 1>), join, dim3(256), 0, s, a);
 }
 
 template <int D>

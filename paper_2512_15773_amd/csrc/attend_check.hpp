@@ -13,7 +13,8 @@ constexpr Fault NO_FAULT{TSDP_OK, nullptr};
 
 constexpr int64_t MOST_ROW = int64_t(1) << 24;       // elements from one row to the next
 constexpr int MOST_HEADS = 1024, MOST_TOKENS = 1024, MOST_GRID_Y = 65535;
-constexpr int64_t MOST_GRID = 0x7FFFFFFF;
+constexpr int64_t MOST_GRID = 0xFFFFFFFF / 512;       // workgroups: a launch has fewer than 2^32 threads, a workgroup up to 512
+constexpr int MOST_LENGTH = 0x7FFFFF00;              // keys: whole tiles of them are counted in 32 bits
 
 inline bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 inline bool head_dim_ok(int d) { return d == 32 || d == 64 || d == 128; }
@@ -60,6 +61,7 @@ inline Fault cache_rows_fault(const tsdp_kv_cache* cache, int B, int R_cap, int 
   Fault f = cache_fault(cache, B);
   if (f.code) return f;
   if (R_cap < 0) return {TSDP_E_SHAPE, "R_cap must not be negative"};
+  if (cache_blocks(R_cap, cache->kv_heads, cache->head_dim) > MOST_GRID) return {TSDP_E_SHAPE, "too many rows for one launch"};
   if (type != 0 && type != 1) return {TSDP_E_INVAL, "rows are fp32 (0) or bf16 (1)"};
   if (B == 0 || R_cap == 0) return NO_FAULT;
   if (!row_ptr || !start) return {TSDP_E_INVAL, "null row table"};
@@ -74,7 +76,7 @@ inline Fault prompt_fault(const tsdp_heads* h, int B, int q_cap, int k_cap, cons
   Fault f = heads_fault(h);
   if (f.code) return f;
   if (B < 0 || q_cap < 0 || k_cap < 0) return {TSDP_E_SHAPE, "B, q_cap and k_cap must not be negative"};
-  if ((int64_t)h->q_heads * ((int64_t)q_cap / 32 + B) > MOST_GRID) return {TSDP_E_SHAPE, "too many rows times heads for one launch"};
+  if (h->q_heads * prompt_slots(q_cap, B, 64) > MOST_GRID || k_cap > MOST_LENGTH) return {TSDP_E_SHAPE, "too many rows times heads for one launch"};
   if (B == 0 || q_cap == 0) return NO_FAULT;
   if (!q_ptr) return {TSDP_E_INVAL, "null row table"};
   if (!k_ptr && k_cap != q_cap) return {TSDP_E_INVAL, "without a row table of the keys k_cap must equal q_cap"};
@@ -89,7 +91,8 @@ inline Fault prompt_fault(const tsdp_heads* h, int B, int q_cap, int k_cap, cons
 inline int64_t scratch_bytes(const tsdp_heads* h, int B, int tokens, int max_len) {
   if (B < 0 || tokens < 1 || tokens > MOST_TOKENS || max_len < 0) return -1;
   const int cols = tokens * (h->q_heads / h->kv_heads), n = most_chunks(max_len, cols);
-  if (n > MOST_GRID_Y || (int64_t)B * h->kv_heads * cols > MOST_GRID) return -1;
+  const int64_t bk = (int64_t)B * h->kv_heads;
+  if (n > MOST_GRID_Y || paged_blocks(bk, cols) > MOST_GRID || join_blocks(bk, cols, n) > MOST_GRID) return -1;
   return n <= 1 ? 0 : (int64_t)B * h->kv_heads * cols * n * (h->head_dim + 2) * 4;
 }
 

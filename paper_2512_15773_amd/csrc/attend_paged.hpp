@@ -466,7 +466,6 @@ __global__ __launch_bounds__(256, 2) void k_paged(PagedArgs a) {
 
 // Adds up the chunks of a column, 16 bytes a lane: D / 4 lanes hold an output, and the lanes of a wave (up to JOIN_ONE chunks) or
 // of four waves (more) so many chunks at a time.  Which, goes by the sequence's own length.
-constexpr int JOIN_ONE = 16;
 template <int D>
 struct PagedJoin {
   static constexpr int LANES = D / 4, SETS = 64 / LANES;         // chunks that a wave's load covers

@@ -74,4 +74,19 @@ inline int most_chunks(int max_len, int cols) {
   return n;
 }
 
+constexpr int JOIN_ONE = 16;                 // chunks that one wave adds up
+
+// Workgroups of the launches of a call: rows of the cache, queries of a prompt, the larger of the two over the cache.
+inline int rows_per_wave(int kv_heads, int head_dim) {           // as many as 64 lanes of 8 elements hold, one at least
+  const int n = 64 / (2 * kv_heads * (head_dim / 8));
+  return n > 1 ? n : 1;
+}
+inline int64_t cache_blocks(int64_t rows, int kv_heads, int head_dim) {
+  const int64_t n = 4 * rows_per_wave(kv_heads, head_dim);
+  return (rows + n - 1) / n;
+}
+inline int64_t prompt_slots(int64_t rows, int64_t B, int tq) { return rows / tq + B; }
+inline int64_t paged_blocks(int64_t bk, int cols) { return cols <= 16 ? bk : bk * ((cols + 63) / 64); }
+inline int64_t join_blocks(int64_t bk, int cols, int chunks) { return chunks <= 1 ? 0 : chunks <= JOIN_ONE ? bk * ((cols + 3) / 4) : bk * cols; }
+
 }  // namespace tsdp

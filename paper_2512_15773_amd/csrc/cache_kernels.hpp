@@ -19,7 +19,7 @@ struct CacheRows {
   const int32_t* row_ptr; const int32_t* start;
   void* k; void* v;                          // packed rows
   int64_t k_row, v_row;                      // elements from one row to the next
-  int per_wave;                              // rows a wave takes: as many as 64 lanes of 8 elements hold, one at least
+  int per_wave;                              // rows a wave takes
   int32_t* status;
 };
 

@@ -196,6 +196,24 @@ def test_refused_paged_calls(plan):
     assert call(good, h=b.TsdpHeads(**{**heads, "type": 0})) == INVAL           # fp32 queries with bf16 outputs
 
 
+def test_refused_launches(plan):
+    """A launch has fewer than 2^32 threads: calls that would need more are refused, not left to the launch."""
+    b, at, heads, cache = _good()
+    most = (2 ** 32 - 1) // 512
+    c, one = b.TsdpKvCache(**{**cache, "B": 2 ** 31 - 1}), b.TsdpHeads(**{**heads, "q_heads": 2})
+    rows = lambda n: plan.refuse_rows(C.byref(c), 4, n, 1, at, at, at, 128, at, 128)
+    assert rows(2 * 4 * most) == OK and rows(2 * 4 * most + 1) == SHAPE          # two rows a wave, four waves
+    prompt = lambda B, q, k: plan.refuse_prompt(C.byref(one), B, q, k, at, at, at, 512, at, 128, at, 128, at, 512)
+    assert prompt(4, 64 * (most // 2 - 4), 100) == OK and prompt(4, 64 * (most // 2 - 3), 100) == SHAPE
+    assert prompt(most // 2, 63, 100) == OK and prompt(most // 2, 64, 100) == SHAPE
+    assert prompt(4, 100, 2 ** 31 - 256) == OK and prompt(4, 100, 2 ** 31 - 255) == SHAPE
+    scratch = lambda B, tokens, n: plan.scratch(C.byref(one), B, tokens, n)      # two kv heads, a column a token
+    assert scratch(most // 2, 16, 256) == 0 and scratch(most // 2 + 1, 16, 256) < 0
+    assert scratch(most // 4, 65, 1024) == 0 and scratch(most // 4 + 1, 65, 1024) < 0
+    assert scratch(most // 8, 16, 300) > 0 and scratch(most // 8 + 1, 16, 300) < 0
+    assert scratch(most // 2, 1, 10000) > 0 and scratch(most // 4, 2, 10000) > 0 and scratch(most // 4 + 1, 2, 10000) < 0
+
+
 def test_oracle_of_8_bits():
     x = ao.e4m3_values()
     assert np.nanmax(x) == 448 and np.isnan(x[[127, 255]]).all() and x[8] == 2.0 ** -6 and x[1] == 2.0 ** -9
