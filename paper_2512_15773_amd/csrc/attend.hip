@@ -102,9 +102,9 @@ void launch_paged(const PagedArgs& a, hipStream_t s) {
   else
     hipLaunchKernelGGL((k_wide<D, HELD, QF32, NP, Out, true, PagedArgs>), dim3((unsigned)paged_blocks(bk, a.cols), a.max_chunks), dim3(256 * WIDE_GROUPS<true>), 0, s, a);
   if (a.max_chunks <= 1) return;
-  const dim3 join((unsigned)join_blocks(bk, a.cols, a.max_chunks));
-  if (a.max_chunks <= JOIN_ONE) hipLaunchKernelGGL((k_paged_join<D, Out, 4>), join, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((k_paged_join<D, Out, 1>), join, dim3(256), 0, s, a);
+  const dim3 join((unsigned)join_blocks(bk, a.cols, a.max_chunks, D));
+  if (a.max_chunks <= JOIN_ONE) hipLaunchKernelGGL((k_paged_join<D, Out, true>), join, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((k_paged_join<D, Out, false>), join, dim3(256), 0, s, a);
 }
 
 template <int D>

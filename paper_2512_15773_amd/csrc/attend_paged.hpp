@@ -464,15 +464,46 @@ __global__ __launch_bounds__(256, 2) void k_paged(PagedArgs a) {
   }
 }
 
-// Adds up the chunks of a column, 16 bytes a lane: D / 4 lanes hold an output, and the lanes of a wave (up to JOIN_ONE chunks) or
-// of four waves (more) so many chunks at a time.  Which, goes by the sequence's own length.
+// Adds up the chunks of a column, 16 bytes a lane: D / 4 lanes hold an output.  Up to JOIN_ONE chunks are added one after the other by
+// the same lanes (64 queries of 32 sequences of 501..4000 tokens, 12 heads of 64: 5.8 us; 11.2 with a wave a column); more by the lanes
+// of four waves, so many chunks at a time.  Which, goes by the sequence's own length.
 template <int D>
 struct PagedJoin {
   static constexpr int LANES = D / 4, SETS = 64 / LANES;         // chunks that a wave's load covers
   f32x4 y = f32x4{};
   float top = -INFINITY, total = 0.f;
-  // chunks first, first + step .. of those at `at`
-  __device__ __forceinline__ void add(const PagedArgs& a, int64_t at, int chunks, int first, int step, int lane) {
+  __device__ __forceinline__ void few(const PagedArgs& a, int64_t at, int chunks, int lane) {
+    const f32x2* ml = reinterpret_cast<const f32x2*>(a.part_ml) + at;
+    const float* p = a.part + at * D + lane * 4;
+    for (int n = 0; n < chunks; n += 4) {
+      f32x2 w[4];
+      f32x4 v[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int c = min(n + u, chunks - 1);
+        w[u] = ml[c];
+        v[u] = *reinterpret_cast<const f32x4*>(p + (int64_t)c * D);
+      }
+      float to = top;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) to = fmaxf(to, w[u][0]);
+      const float sub = to == -INFINITY ? 0.f : to, by = __builtin_amdgcn_exp2f(top - sub);
+      total *= by;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] *= by;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (n + u >= chunks) break;
+        const float f = __builtin_amdgcn_exp2f(w[u][0] - sub);
+        total = fmaf(w[u][1], f, total);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = fmaf(v[u][e], f, y[e]);
+      }
+      top = to;
+    }
+  }
+  // every SETS * 4-th of many chunks
+  __device__ __forceinline__ void many(const PagedArgs& a, int64_t at, int chunks, int wave, int lane) {
     const float* ml = a.part_ml + 2 * at;
     for (int n = lane; n < chunks; n += 64) top = fmaxf(top, ml[2 * n]);
 #pragma unroll
@@ -480,7 +511,7 @@ struct PagedJoin {
     const float sub = top == -INFINITY ? 0.f : top;
     const float* p = a.part + at * D + (lane % LANES) * 4;
 #pragma unroll 4
-    for (int n = first + lane / LANES; n < chunks; n += step) {
+    for (int n = wave * SETS + lane / LANES; n < chunks; n += 4 * SETS) {
       const float f = __builtin_amdgcn_exp2f(ml[2 * n] - sub);
       const f32x4 v = *reinterpret_cast<const f32x4*>(p + (int64_t)n * D);
       total = fmaf(ml[2 * n + 1], f, total);
@@ -494,41 +525,48 @@ struct PagedJoin {
       for (int e = 0; e < 4; ++e) y[e] += __shfl_xor(y[e], s);
     }
   }
+  template <typename Out>
+  __device__ __forceinline__ void out(const PagedArgs& a, int b, int kvh, int col, int lane) const {
+    const int G = a.heads / a.cache.kv_heads, head = kvh * G + col % G;
+    const int64_t row = (int64_t)b * a.tokens + col / G;
+    Out* to = static_cast<Out*>(a.out) + row * a.out_row + head * D + lane * 4;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) to[e] = (Out)(total == 0.f ? 0.f : y[e] / total);
+    if (a.lse && lane == 0) a.lse[row * a.heads + head] = (top + __builtin_amdgcn_logf(total)) * LN2;
+  }
 };
 
-// PER columns a workgroup: four where no sequence of the call can have more than JOIN_ONE chunks.
-template <int D, typename Out, int PER>
+// FEW: no sequence of the call can have more than JOIN_ONE chunks; a workgroup takes as many columns as it has lanes for.  Otherwise
+// one column.
+template <int D, typename Out, bool FEW>
 __global__ __launch_bounds__(256) void k_paged_join(PagedArgs a) {
   typedef PagedJoin<D> Join;
-  __shared__ __align__(16) float lds[4][D + 4];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, G = a.heads / a.cache.kv_heads, kv = a.cache.kv_heads;
-  const int groups = (a.cols + PER - 1) / PER, kvh = blockIdx.x / groups % kv, b = blockIdx.x / groups / kv;
-  const int len = paged_len(a, b), chunks = chunks_of(len, a.cols);
-  const bool alone = PER == 4 || chunks <= JOIN_ONE;
-  const int col = blockIdx.x % groups * PER + (PER == 4 ? wave : 0);
-  if (chunks <= 1 || col >= a.cols || (PER == 1 && alone && wave > 0)) return;
-  const int64_t at = (((int64_t)b * kv + kvh) * a.cols + col) * a.max_chunks;
+  const int kv = a.cache.kv_heads, lane = threadIdx.x % Join::LANES;
+  const int64_t column = FEW ? (int64_t)blockIdx.x * join_columns(D) + threadIdx.x / Join::LANES : blockIdx.x;
+  if (column >= (int64_t)a.B * kv * a.cols) return;
+  const int col = (int)(column % a.cols), bk = (int)(column / a.cols), b = bk / kv;
+  const int chunks = chunks_of(paged_len(a, b), a.cols);
+  if (chunks <= 1) return;
+  const int64_t at = column * a.max_chunks;
   Join j;
-  j.add(a, at, chunks, alone ? 0 : wave * Join::SETS, alone ? Join::SETS : 4 * Join::SETS, lane);
-  if (!alone) {
-    if (lane < Join::LANES) *reinterpret_cast<f32x4*>(&lds[wave][4 * lane]) = j.y;
-    if (lane == 0) lds[wave][D] = j.total;
+  if (FEW || chunks <= JOIN_ONE) {
+    if (!FEW && threadIdx.x >= Join::LANES) return;
+    j.few(a, at, chunks, lane);
+  } else {
+    __shared__ __align__(16) float lds[4][D + 4];
+    const int wave = threadIdx.x >> 6;
+    j.many(a, at, chunks, wave, threadIdx.x & 63);
+    if ((threadIdx.x & 63) < Join::LANES) *reinterpret_cast<f32x4*>(&lds[wave][4 * lane]) = j.y;
+    if ((threadIdx.x & 63) == 0) lds[wave][D] = j.total;
     __syncthreads();
-    if (wave > 0) return;
+    if (threadIdx.x >= Join::LANES) return;
     j.y = f32x4{}; j.total = 0.f;
     for (int w = 0; w < 4; ++w) {
       j.total += lds[w][D];
-      if (lane < Join::LANES) j.y += *reinterpret_cast<const f32x4*>(&lds[w][4 * lane]);
+      j.y += *reinterpret_cast<const f32x4*>(&lds[w][4 * lane]);
     }
   }
-  const int head = kvh * G + col % G;
-  const int64_t row = (int64_t)b * a.tokens + col / G;
-  Out* out = static_cast<Out*>(a.out) + row * a.out_row + head * D + lane * 4;
-  if (lane < Join::LANES) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) out[e] = (Out)(j.total == 0.f ? 0.f : j.y[e] / j.total);
-  }
-  if (a.lse && lane == 0) a.lse[row * a.heads + head] = (j.top + __builtin_amdgcn_logf(j.total)) * LN2;
+  j.template out<Out>(a, b, bk % kv, col, lane);
 }
 
 }  // namespace tsdp

@@ -74,7 +74,8 @@ inline int most_chunks(int max_len, int cols) {
   return n;
 }
 
-constexpr int JOIN_ONE = 16;                 // chunks that one wave adds up
+constexpr int JOIN_ONE = 16;                 // chunks that the same lanes add up
+TSDP_HD constexpr int join_columns(int head_dim) { return 256 / (head_dim / 4); }   // columns of a workgroup of such lanes
 
 // Workgroups of the launches of a call: rows of the cache, queries of a prompt, the larger of the two over the cache.
 inline int rows_per_wave(int kv_heads, int head_dim) {           // as many as 64 lanes of 8 elements hold, one at least
@@ -87,6 +88,9 @@ inline int64_t cache_blocks(int64_t rows, int kv_heads, int head_dim) {
 }
 inline int64_t prompt_slots(int64_t rows, int64_t B, int tq) { return rows / tq + B; }
 inline int64_t paged_blocks(int64_t bk, int cols) { return cols <= 16 ? bk : bk * ((cols + 63) / 64); }
-inline int64_t join_blocks(int64_t bk, int cols, int chunks) { return chunks <= 1 ? 0 : chunks <= JOIN_ONE ? bk * ((cols + 3) / 4) : bk * cols; }
+inline int64_t join_blocks(int64_t bk, int cols, int chunks, int head_dim) {
+  const int64_t columns = bk * cols, per = join_columns(head_dim);
+  return chunks <= 1 ? 0 : chunks <= JOIN_ONE ? (columns + per - 1) / per : columns;
+}
 
 }  // namespace tsdp

@@ -210,7 +210,7 @@ def test_refused_launches(plan):
     scratch = lambda B, tokens, n: plan.scratch(C.byref(one), B, tokens, n)      # two kv heads, a column a token
     assert scratch(most // 2, 16, 256) == 0 and scratch(most // 2 + 1, 16, 256) < 0
     assert scratch(most // 4, 65, 1024) == 0 and scratch(most // 4 + 1, 65, 1024) < 0
-    assert scratch(most // 8, 16, 300) > 0 and scratch(most // 8 + 1, 16, 300) < 0
+    assert scratch(most // 2, 16, 300) > 0 and scratch(most // 2 + 1, 16, 300) < 0
     assert scratch(most // 2, 1, 10000) > 0 and scratch(most // 4, 2, 10000) > 0 and scratch(most // 4 + 1, 2, 10000) < 0
 
 
