@@ -76,6 +76,14 @@ __device__ __forceinline__ bool not_finite_bf16(uint32_t w) {
 __device__ __forceinline__ uint32_t not_finite_halves(uint32_t w) {   // bit 0: the low half, bit 1: the high one
   return ((w & 0x7F80u) == 0x7F80u ? 1u : 0u) | ((w & 0x7F800000u) == 0x7F800000u ? 2u : 0u);
 }
+// whether one of eight is not finite
+__device__ __forceinline__ bool some_not_finite(u32x4 w) {
+  typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
+  u16x2 most = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, w[i] & 0x7FFF7FFFu));
+  return most[0] >= 0x7F80u || most[1] >= 0x7F80u;
+}
 // both halves: 0 where finite, 1.0 where not; and the word with such halves taken out
 __device__ __forceinline__ uint32_t marks_bf16(uint32_t w) {
   return ((w & 0x7F80u) == 0x7F80u ? 0x3F80u : 0u) | ((w & 0x7F800000u) == 0x7F800000u ? 0x3F800000u : 0u);

@@ -214,6 +214,7 @@ __global__ __launch_bounds__(NW * 64, WAVES) void k_prompt_bf16(PromptArgs a) {
   const int tiles = (seen(min(t.i0 + C::TQ, t.nq) - 1, t.nq, t.nk, a.causal) + KT - 1) / KT;
   const int mine = i < t.nq ? seen(i, t.nq, t.nk, a.causal) : 0;                              // keys that this lane's query sees
   const int some = i0 < t.nq ? seen(min(i0 + 31, t.nq - 1), t.nq, t.nk, a.causal) : 0;        // and that some query of the wave sees
+  const int least = seen(i0, t.nq, t.nk, a.causal);            // and that every query of it sees
   if (lane == 0) { unusual[wave] = 0; rises[wave] = 0; }
 
   const __bf16* kb = static_cast<const __bf16*>(a.k) + (int64_t)t.k_lo * a.k_row + t.kv_head * D;
@@ -328,17 +329,19 @@ __global__ __launch_bounds__(NW * 64, WAVES) void k_prompt_bf16(PromptArgs a) {
       u32x4* at = reinterpret_cast<u32x4*>(v + (x * NW + wave) * 1024 + lane * 16);
       u32x4 y = *at;
       uint32_t marks = 0;
-#pragma unroll
-      for (int z = 0; z < 4; ++z) marks |= not_finite_halves(y[z]) << (2 * z);
-      where[n & 1][(x * C::RPR + sr) * CH + (pc ^ value_swizzle<CH>(sr))] = (uint8_t)marks;
-      if (marks) {
+      if (__any(some_not_finite(y))) {
         bad = true;
 #pragma unroll
-        for (int z = 0; z < 4; ++z) y[z] = finite_bf16(y[z]);
-        *at = y;
+        for (int z = 0; z < 4; ++z) marks |= not_finite_halves(y[z]) << (2 * z);
+        if (marks) {
+#pragma unroll
+          for (int z = 0; z < 4; ++z) y[z] = finite_bf16(y[z]);
+          *at = y;
+        }
       }
+      where[n & 1][(x * C::RPR + sr) * CH + (pc ^ value_swizzle<CH>(sr))] = (uint8_t)marks;
     }
-    if (__any(bad) && lane == 0) unusual[wave] = 1;
+    if (bad && lane == 0) unusual[wave] = 1;
     __syncthreads();
     if (n > from) TSDP_KEYS(n + 1, kn);
     TSDP_VALUES(n + 1, vn);
@@ -348,9 +351,11 @@ __global__ __launch_bounds__(NW * 64, WAVES) void k_prompt_bf16(PromptArgs a) {
       if (n * KT + 32 * u >= some) continue;
       f32x16 s = w.scores(k, 32 * u, lane);
       bf16x8 p[2];
+      if (n * KT + 32 * u + 32 > least) {
 #pragma unroll
-      for (int x = 0; x < 16; ++x)
-        if (8 * (x / 4) + 4 * half + x % 4 >= left) s[x] = -INFINITY;
+        for (int x = 0; x < 16; ++x)
+          if (8 * (x / 4) + 4 * half + x % 4 >= left) s[x] = -INFINITY;
+      }
       float f;
       if (__any(w.maximum(s, a.c, f))) w.scale(f);
       const float sub = w.subtrahend();
