@@ -10,6 +10,9 @@
 // when the value operand takes its keys in that order.  A lane loads D / 16 neighbouring values of those eight keys (whole
 // rows per 16 lanes) and turns them with byte permutes into D / 16 operands, operand f holding dims (D / 16) r + f.
 //
+// Measured: 8 sequences of 20001..131072 tokens, 32 / 8 heads of 128 in 8 bits, 259 us = 5.2 TB/s (a large read reaches 5.9); 256 of
+// 1..2001, 8 / 2 heads of 64 in bf16, 26 us = 5.1 TB/s; the join 4 to 6 us.
+//
 // Fewer than 32 bits enter a matrix product only without loss: keys and values as they are held (8 bits widen exactly to
 // bf16 with their scale), fp32 queries as three bf16 parts, and the weights P as two or three (to 2^-16 or 2^-24 of each).
 #pragma once
@@ -37,8 +40,8 @@ __device__ __forceinline__ int paged_len(const PagedArgs& a, int b) {
   return n < 0 ? 0 : (int)min((long)n, room);
 }
 
+// 32 keys and values of a kv head in registers, as they are held
 template <int D, int HELD> struct PagedTile;
-
 
 template <int D> struct PagedTile<D, HELD_BF16> {
   u32x4 k[2][D / 32];
@@ -351,7 +354,9 @@ struct PagedWave {
 template <int D, int HELD, bool QF32, int NP, typename Out>
 __global__ __launch_bounds__(256, 2) void k_paged(PagedArgs a) {
   constexpr int F = D / 16, OP = D + 4;
-  constexpr bool AHEAD = !(HELD == HELD_F32 && D == 128);        // registers hold two tiles
+  // The next tile is loaded ahead where registers hold two (12 heads on one of 64 in fp32, 32 sequences of 2000: 16.1 us, 18.1 without;
+  // 8 sequences of 20001..131072, 32 / 8 heads of 128 in 8 bits: 259 and 263; 256 of 1..2001, 8 / 2 heads of 64 in bf16: 25.8 and 26.5).
+  constexpr bool AHEAD = !(HELD == HELD_F32 && D == 128);
   __shared__ __align__(16) float o_lds[4][16][OP];
   __shared__ float ml_lds[4][16][2];
   const int kv = a.cache.kv_heads, kvh = blockIdx.x % kv, b = blockIdx.x / kv, chunk = blockIdx.y;
@@ -464,7 +469,7 @@ __global__ __launch_bounds__(256, 2) void k_paged(PagedArgs a) {
   }
 }
 
-// Adds up the chunks of a column, 16 bytes a lane: D / 4 lanes hold an output.  Up to JOIN_ONE chunks are added one after the other by
+// Adds up the chunks of a column, 16 bytes a lane: D / 4 lanes hold an output.  Up to join_one chunks are added one after the other by
 // the same lanes (64 queries of 32 sequences of 501..4000 tokens, 12 heads of 64: 5.8 us; 11.2 with a wave a column); more by the lanes
 // of four waves, so many chunks at a time.  Which, goes by the sequence's own length.
 template <int D>
@@ -536,7 +541,7 @@ struct PagedJoin {
   }
 };
 
-// FEW: no sequence of the call can have more than JOIN_ONE chunks; a workgroup takes as many columns as it has lanes for.  Otherwise
+// FEW: no sequence of the call can have more than join_one chunks; a workgroup takes as many columns as it has lanes for.  Otherwise
 // one column.
 template <int D, typename Out, bool FEW>
 __global__ __launch_bounds__(256) void k_paged_join(PagedArgs a) {
@@ -549,7 +554,7 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedArgs a) {
   if (chunks <= 1) return;
   const int64_t at = column * a.max_chunks;
   Join j;
-  if (FEW || chunks <= JOIN_ONE) {
+  if (FEW || chunks <= join_one(a.cols)) {
     if (!FEW && threadIdx.x >= Join::LANES) return;
     j.few(a, at, chunks, lane);
   } else {

@@ -9,6 +9,11 @@
 // the bf16 matrix pipe take 3/8 of the time of one of the fp32 pipe.  8 bits are one part, their scale included.  Weights are three parts
 // for outputs in fp32, two for bf16.
 //
+// Bound by the vector and LDS pipes of workgroups that run for different times (ragged lengths), not by memory: 64 queries of 32
+// sequences of 501..4000 tokens, 12 / 4 heads of 64 in 8 bits, outputs in fp32: 64 us = 225 TFLOP/s of the two products (each weight is
+// multiplied in three parts; matrix pipe busy 18 %, vector pipe 40 %, 2 of 3 waves a SIMD resident on average); the fp32 prompts
+// above: 64 us = 87 TFLOP/s (matrix 23 %, vector 39 %).
+//
 // The operand layouts are those of the narrow kernel: S^T = K Q^T, O^T = V^T P^T in tiles of 16, P in registers throughout.
 // The maximum is that of the first keys, as everywhere; a rise is noticed from the sums, and the workgroup starts over with
 // maxima that move.
@@ -123,8 +128,12 @@ struct Wide {
   typedef WideRow<D, HELD> Row;
   static constexpr int KT = 32, NK = Row::NK, NQ = QF32 ? 3 : 1, F = D / 16, CH = D / 8, E = Row::E, PLANE = KT * D * 2;
   static constexpr int BYTES = 2 * NK * PLANE;                   // keys, values
+  // Two buffers save a barrier a tile where LDS has room for as many workgroups (64 queries of 32 sequences of 2000 tokens, 12 / 4 heads
+  // of 64 in 8 bits: 51.5 us, 52.8 with one; prompts of 32 x 200, 8 heads of 32 in fp32: 23.8 and 25.0).
   static constexpr int BUFFERS = BYTES <= 16 * 1024 ? 2 : 1;
-  static constexpr int AHEAD = NK == 1 ? 4 : 1;                   // tiles in registers on their way
+  // Tiles in registers on their way: one in fp32, whose conversion leaves no registers, otherwise four (51.5 us, 52.9 with two; 8
+  // sequences of 2000, 64 queries, 32 / 8 heads of 128 in bf16: 50.9 and 53.2).
+  static constexpr int AHEAD = NK == 1 ? 4 : 1;
 
   f32x4 o[F];
   bf16x8 q[NQ][D / 32];

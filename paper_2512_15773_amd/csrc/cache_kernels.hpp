@@ -2,6 +2,8 @@
 //
 // Both kernels are one pass over the data, bound by HBM: a wave takes one token's row of keys and values (several, where they
 // are short), finds the environment that the row belongs to and the page of its position, and moves 8 elements a lane and step.
+// Measured: 8 sequences of 9001..16384 tokens, 8 heads of 128, bf16 rows into 8 bits 137 us = 4.5 TB/s, and back 125 us = 5.0 TB/s (a
+// large copy: 5.1); 65536 rows of one head of 32: 8.7 us and 7.2 (19.3 and 16.9 with a row a wave).
 //
 // 8 bits (gfx950 converts to and from them in one instruction): blocks of 32 elements along a head share one power of two,
 // the smallest 2^e with max|x| <= 448 * 2^e, and are held as e4m3 of x * 2^-e, rounded to the nearest, ties to even.  The

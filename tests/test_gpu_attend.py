@@ -350,6 +350,27 @@ def test_paged_long(ctx, dtype, held):
     assert ctx.tsdp_status() == 0
 
 
+@pytest.mark.parametrize("dtype,held", (("fp32", "fp32"), ("bf16", "mx8")))
+def test_paged_long_many_columns(ctx, dtype, held):
+    """As above for 36 columns, on both sides of the chunks that one set of lanes joins."""
+    import torch
+    rng = np.random.default_rng(18)
+    lens, tokens = [16384, 17500, 16385, 5, 1025], 9
+    c, values = filled(rng, held, lens, 1, 256, 64)
+    q = draw(rng, (len(lens) * tokens, 4, 64), dtype)
+    lse = torch.zeros(len(lens) * tokens, 4, device="cuda")
+    got = ctx.tsdp_attend_paged(q, c, i32(lens), 17500, tokens=tokens, lse=lse)
+    for b, n in enumerate(lens):
+        r = slice(b * tokens, (b + 1) * tokens)
+        check(got[r], lse[r], ao.attend(f64(q[r]), values[0][b], values[1][b], 0.125, True), 64, n, dtype, WEIGHTS["paged"][dtype], n)
+    from paper_2512_15773_amd import KvCache
+    for b in (0, 2, 4):
+        one, r = KvCache(c.k, c.v, c.page_table[b:b + 1], c.k_scale, c.v_scale), slice(b * tokens, (b + 1) * tokens)
+        for most in (lens[b], 60000):
+            assert torch.equal(ctx.tsdp_attend_paged(q[r], one, i32([lens[b]]), most, tokens=tokens), got[r]), (b, most)
+    assert ctx.tsdp_status() == 0
+
+
 @pytest.mark.parametrize("held", ("bf16", "mx8"))
 def test_pools_past_32_bits(ctx, held):
     """The last pages of pools of more than 2^32 bytes (8 bits) and 2^32 elements' bytes: written, attended to and read back."""
