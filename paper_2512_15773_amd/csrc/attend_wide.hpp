@@ -11,7 +11,7 @@
 //
 // Bound by the vector and LDS pipes of workgroups that run for different times (ragged lengths), not by memory: 64 queries of 32
 // sequences of 501..4000 tokens, 12 / 4 heads of 64 in 8 bits, outputs in fp32: 64 us = 225 TFLOP/s of the two products (each weight is
-// multiplied in three parts; matrix pipe busy 18 %, vector pipe 40 %, 2 of 3 waves a SIMD resident on average); the fp32 prompts
+// multiplied in three parts; matrix pipe busy 18 %, vector pipe 40 %, 1.8 of 4 waves a SIMD resident on average); the fp32 prompts
 // above: 64 us = 87 TFLOP/s (matrix 23 %, vector 39 %).
 //
 // The operand layouts are those of the narrow kernel: S^T = K Q^T, O^T = V^T P^T in tiles of 16, P in registers throughout.
