@@ -4,14 +4,14 @@
 // A workgroup takes 64 columns and all keys of them (of its chunk), 32 keys at a time: they are loaded into registers some tiles
 // ahead, turned into bf16 once for all columns and put into LDS; each of four waves owns 16 columns.  Prompts have two such groups
 // of waves, which take tiles in turns and join at the end: half the way from the first key to the last (71 -> 64 us for four prompts
-// of 301..1501 tokens, 8 heads of 64; over the cache, whose chunks are short, one group is faster by 14 % on ragged lengths).  fp32 becomes three bf16
-// parts that add up to it exactly to 2^-24, and a product of fp32 six products of parts (what is left out is 2^-25 of it each): 6 passes of
+// of 301..1501 tokens, 8 heads of 64; over the cache, whose chunks are short, one group is faster by 14 % on ragged lengths).  fp32 becomes
+// three bf16 parts that add up to it to 2^-24, and a product of fp32 six products of parts (what is left out is 2^-25 of it each): 6 passes of
 // the bf16 matrix pipe take 3/8 of the time of one of the fp32 pipe.  8 bits are one part, their scale included.  Weights are three parts
 // for outputs in fp32, two for bf16.
 //
 // Bound by the vector and LDS pipes of workgroups that run for different times (ragged lengths), not by memory: 64 queries of 32
-// sequences of 501..4000 tokens, 12 / 4 heads of 64 in 8 bits, outputs in fp32: 64 us = 225 TFLOP/s of the two products (each weight is
-// multiplied in three parts; matrix pipe busy 18 %, vector pipe 40 %, 1.8 of 4 waves a SIMD resident on average); the fp32 prompts
+// sequences of 501..4000 tokens, 12 / 4 heads of 64 in 8 bits, outputs in fp32: 60.5 us = 240 TFLOP/s of the two products (each weight is
+// multiplied in three parts; vector pipe busy 40 %, 1.8 of 4 waves a SIMD resident on average); the fp32 prompts
 // above: 64 us = 87 TFLOP/s (matrix 23 %, vector 39 %).
 //
 // The operand layouts are those of the narrow kernel: S^T = K Q^T, O^T = V^T P^T in tiles of 16, P in registers throughout.
@@ -134,6 +134,11 @@ struct Wide {
   // Tiles in registers on their way: one in fp32, whose conversion leaves no registers, otherwise four (51.5 us, 52.9 with two; 8
   // sequences of 2000, 64 queries, 32 / 8 heads of 128 in bf16: 50.9 and 53.2).
   static constexpr int AHEAD = NK == 1 ? 4 : 1;
+  // Over the cache, tiles without masks: the scores of the next tile while the weights of this one are made, so that the matrix pipe does
+  // not wait for the exponentials.  Keys go to LDS a tile before values, into the other buffer (64 queries of 32 sequences of 501..4000
+  // tokens, 12 / 4 heads of 64 in 8 bits: 60.5 us, 64.2 one after the other; 4 of 16000, 32 / 8 heads of 128 in bf16: 169 and 187).
+  static constexpr bool PIPE = NK == 1;
+  static_assert(!PIPE || (AHEAD % 2 == 0 && BUFFERS == 2), "buffers go in turns with the tiles");
 
   f32x4 o[F];
   bf16x8 q[NQ][D / 32];
@@ -182,11 +187,10 @@ struct Wide {
     }
   }
 
-  // The 32 keys of a tile.  careful: some are masked (sees), or maxima have to be looked at.
-  template <class Sees>
-  __device__ __forceinline__ void step(const uint8_t* keys, const uint8_t* values, float c, int lane, bool careful, bool masked, Sees sees) {
+  // of the 32 keys of a tile
+  __device__ __forceinline__ void scores(f32x4 (&s)[2], const uint8_t* keys, int lane) const {
     const int r = lane & 15, g = lane >> 4;
-    f32x4 s[2] = {f32x4{}, f32x4{}};
+    s[0] = f32x4{}; s[1] = f32x4{};
 #pragma unroll
     for (int x = 0; x < D / 32; ++x)
 #pragma unroll
@@ -201,14 +205,24 @@ struct Wide {
           for (int z = 0; z < NK; ++z)
             if (sum - z >= 0 && sum - z < NQ) s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[z], q[sum - z][x], s[u], 0, 0, 0);
       }
+  }
+  static __device__ __forceinline__ float largest(const f32x4 (&s)[2]) {
+    const float top = max3(max3(s[0][0], s[0][1], s[0][2]), s[0][3], s[1][0]);
+    return max_groups(max3(max3(top, s[1][1], s[1][2]), s[1][3], s[1][3]));
+  }
+  // A tile's scores, weights and product.  careful: some keys are masked (sees), or maxima have to be looked at.
+  template <class Sees>
+  __device__ __forceinline__ void step(const uint8_t* keys, const uint8_t* values, float c, int lane, bool careful, bool masked, Sees sees) {
+    const int g = lane >> 4;
+    f32x4 s[2];
+    scores(s, keys, lane);
     if (careful) {
       if (masked) {
 #pragma unroll
         for (int x = 0; x < 8; ++x)
           if (!sees(16 * (x / 4) + 4 * g + x % 4)) s[x / 4][x % 4] = -INFINITY;
       }
-      float top = max3(max3(s[0][0], s[0][1], s[0][2]), s[0][3], s[1][0]);
-      top = max_groups(max3(max3(top, s[1][1], s[1][2]), s[1][3], s[1][3])) * c;
+      const float top = largest(s) * c;
       const float to = top > m + MOST_RISE ? top : m, f = to == m ? 1.f : __builtin_amdgcn_exp2f(m - to);
       m = to;
       l *= f;
@@ -217,6 +231,29 @@ struct Wide {
 #pragma unroll
         for (int x = 0; x < 4; ++x) o[y][x] *= f;
     }
+    product(s, values, c, lane);
+  }
+  // value operand f: one read turns 4 keys x 16 dims for 16 lanes, each of which names 4 dims of one key
+  static __device__ __forceinline__ void operand(bf16x8 (&v)[NK], const uint8_t* values, int f, int lane) {
+    typedef __attribute__((ext_vector_type(4))) short s16x4;
+    typedef __attribute__((address_space(3))) s16x4* at;
+    const int r = lane & 15, g = lane >> 4, row = 4 * g + (r >> 2), dim = 16 * f + (r & 3) * 4;
+#pragma unroll
+    for (int z = 0; z < NK; ++z) {
+      const uint8_t* base = values + z * PLANE + (dim & 7) * 2;
+      const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)(base + row * (D * 2) + (((dim >> 3) ^ wide_swizzle<CH>(row)) << 4))));
+      const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)(base + (row + 16) * (D * 2) + (((dim >> 3) ^ wide_swizzle<CH>(row + 16)) << 4))));
+      v[z] = __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
+    }
+  }
+  // Weights of scores, and their product with the values.  Where registers allow, two operands are read before the weights are made (8
+  // sequences of 4096, 16 queries, 32 / 8 heads of 128 in 8 bits: 34.0 us, 37.9 without).
+  static constexpr int EARLY = NK == 1 ? 2 : 0;
+  __device__ __forceinline__ void product(const f32x4 (&s)[2], const uint8_t* values, float c, int lane) {
+    bf16x8 v[F][NK];
+#pragma unroll
+    for (int f = 0; f < EARLY; ++f) operand(v[f], values, f, lane);
+    if (EARLY) __builtin_amdgcn_sched_barrier(0);
     const float sub = m == -INFINITY ? 0.f : m;
     bf16x8 p[NP];
 #pragma unroll
@@ -229,25 +266,14 @@ struct Wide {
 #pragma unroll
       for (int z = 0; z < NP; ++z) { p[z][x] = parts[z][0]; p[z][x + 1] = parts[z][1]; }
     }
-    typedef __attribute__((ext_vector_type(4))) short s16x4;
-    typedef __attribute__((address_space(3))) s16x4* at;
-    const int row = 4 * g + (r >> 2);        // one read turns 4 keys x 16 dims for 16 lanes, each of which names 4 dims of one key
 #pragma unroll
     for (int f = 0; f < F; ++f) {
-      bf16x8 v[NK];
-      const int dim = 16 * f + (r & 3) * 4;
-#pragma unroll
-      for (int z = 0; z < NK; ++z) {
-        const uint8_t* base = values + z * PLANE + (dim & 7) * 2;
-        const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)(base + row * (D * 2) + (((dim >> 3) ^ wide_swizzle<CH>(row)) << 4))));
-        const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)(base + (row + 16) * (D * 2) + (((dim >> 3) ^ wide_swizzle<CH>(row + 16)) << 4))));
-        v[z] = __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
-      }
+      if (f + EARLY < F) operand(v[f + EARLY], values, f + EARLY, lane);
 #pragma unroll
       for (int sum = NK + NP - 2 < 2 ? NK + NP - 2 : 2; sum >= 0; --sum)
 #pragma unroll
         for (int z = 0; z < NK; ++z)
-          if (sum - z >= 0 && sum - z < NP) o[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[z], p[sum - z], o[f], 0, 0, 0);
+          if (sum - z >= 0 && sum - z < NP) o[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[f][z], p[sum - z], o[f], 0, 0, 0);
     }
   }
 };
@@ -274,9 +300,11 @@ __device__ __forceinline__ void wide_out(const W& w, __bf16* out, float l, int g
 }
 
 // PAGED: the columns of a kv head over a chunk of the cache; otherwise the queries of a head over their sequence's rows.
+// Waves a SIMD: as many as registers allow; heads of 64 over the cache are held to the 128 of four (64 queries of 32 sequences of 4000
+// tokens, 12 / 4 heads in 8 bits, the call: 79.7 us, 83.2 with the 130 of three), but for queries of three parts, which need 146.
 template <bool PAGED> constexpr int WIDE_GROUPS = PAGED ? 1 : 2;
 template <int D, int HELD, bool QF32, int NP, typename Out, bool PAGED, typename Args>
-__global__ __launch_bounds__(256 * WIDE_GROUPS<PAGED>, (D == 128 ? 2 : PAGED ? 3 : 4)) void k_wide(Args a) {
+__global__ __launch_bounds__(256 * WIDE_GROUPS<PAGED>, (D == 128 ? 2 : PAGED && QF32 ? 3 : 4)) void k_wide(Args a) {
   constexpr int GROUPS = WIDE_GROUPS<PAGED>, WAVES = 4 * GROUPS;
   typedef Wide<D, HELD, QF32, NP> W;
   constexpr int COLS = 64;
@@ -336,15 +364,21 @@ __global__ __launch_bounds__(256 * WIDE_GROUPS<PAGED>, (D == 128 ? 2 : PAGED ? 3
   Row rk[AHEAD], rv[AHEAD];                  // tiles on their way
   uint32_t k_off = 0, v_off = 0;             // !PAGED: this thread's bytes of a tile (a row is at most 2^24 elements)
   if constexpr (!PAGED) { k_off = (my_row * (uint32_t)a.k_row + part * W::E) * 4; v_off = (my_row * (uint32_t)a.v_row + part * W::E) * 4; }
+  // keys or values of tile n of the cache
+  auto load_one = [&](Row& r, const void* pool, const uint8_t* scales, int n) __attribute__((always_inline)) {
+    if constexpr (PAGED) {
+      if (n >= tiles) return;
+      const int page = max(__builtin_amdgcn_readlane(pages, 2 * n + (wave >> 1)), 0);
+      r.load(pool, scales, pool_row(a.cache, page, kvh, (int)((lo + KT * n + 16 * (wave >> 1)) & ((1 << a.cache.page_shift) - 1))), tid & 127);
+    }
+  };
   // the group's tile i is tile GROUPS i + group
   auto load = [&](Row& rk, Row& rv, int i) __attribute__((always_inline)) {
     const int n = GROUPS * i + group;
     if (n >= tiles) return;
     if constexpr (PAGED) {
-      const int page = max(__builtin_amdgcn_readlane(pages, 2 * n + (wave >> 1)), 0);
-      const int64_t row = pool_row(a.cache, page, kvh, (int)((lo + KT * n + 16 * (wave >> 1)) & ((1 << a.cache.page_shift) - 1)));
-      rk.load(a.cache.k, a.cache.k_scale, row, tid & 127);
-      rv.load(a.cache.v, a.cache.v_scale, row, tid & 127);
+      load_one(rk, a.cache.k, a.cache.k_scale, n);
+      load_one(rv, a.cache.v, a.cache.v_scale, n);
     } else {
       const char* ka = reinterpret_cast<const char*>(static_cast<const float*>(a.k) + (int64_t)(t.k_lo + KT * n) * a.k_row + kvh * D);
       const char* va = reinterpret_cast<const char*>(static_cast<const float*>(a.v) + (int64_t)(t.k_lo + KT * n) * a.v_row + kvh * D);
@@ -408,8 +442,45 @@ __global__ __launch_bounds__(256 * WIDE_GROUPS<PAGED>, (D == 128 ? 2 : PAGED ? 3
       }
     }
   };
+  int from = 0;                              // first tile of the loop that looks at masks and maxima
+  if constexpr (W::PIPE && PAGED) if (plain > 0) {
+    f32x4 s[2][2];
+    W::put(rk[0], lds[0], my_row, part, false);
+    load_one(rk[0], a.cache.k, a.cache.k_scale, AHEAD);
+    __syncthreads();
+    w.scores(s[0], lds[0], lane);
+    const float top = W::largest(s[0]) * a.c;
+    w.m = top > -INFINITY ? top : -INFINITY;
+    for (int n = 0; n < plain; n += AHEAD) {
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        if (n + u >= plain) break;
+        W::put(rv[u], lds[u % 2] + W::BYTES / 2, my_row, part, true);
+        load_one(rv[u], a.cache.v, a.cache.v_scale, n + u + AHEAD);
+        if (n + u + 1 < plain) {
+          W::put(rk[(u + 1) % AHEAD], lds[(u + 1) % 2], my_row, part, false);
+          load_one(rk[(u + 1) % AHEAD], a.cache.k, a.cache.k_scale, n + u + 1 + AHEAD);
+          __syncthreads();
+          w.scores(s[(u + 1) % 2], lds[(u + 1) % 2], lane);
+        } else {
+          __syncthreads();
+        }
+        w.product(s[u % 2], lds[u % 2] + W::BYTES / 2, a.c, lane);
+      }
+    }
+    careful = true;
+    from = plain;
+    if (__any(w.l > most_sum(w.m)) && lane == 0) rises[wave8] = 1;
+    __syncthreads();
+    if (any_of<WAVES>(rises)) {                // once more, with maxima that move
+      w.clear();
+      from = 0;
+    }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) load(rk[u], rv[u], from + u);
+  }
   const int steps = (tiles + GROUPS - 1) / GROUPS, steps_plain = (plain + GROUPS - 1) / GROUPS;
-  for (int i = 0; i < steps; i += AHEAD) {
+  for (int i = from; i < steps; i += AHEAD) {
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
       if (i + u >= steps) break;
