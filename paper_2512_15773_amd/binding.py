@@ -7,7 +7,6 @@ Calls only enqueue work on the given (default: torch's current) stream.  The bin
 handed to a call must stay alive until that stream has run the call -- torch's caching allocator does not know of the
 use and would hand a freed tensor's memory out again (keep a reference, or call Tensor.record_stream yourself).
 """
-import contextlib
 import ctypes as C
 import os
 
@@ -114,12 +113,12 @@ def _stream(stream):
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) if stream is None else stream.cuda_stream
 
 
-_CURRENT = contextlib.nullcontext()
-
-
-def _memory_on(stream):
-    """What is allocated inside belongs to the stream that the call runs on: nothing that another stream still uses."""
-    return _CURRENT if stream is None else torch.cuda.stream(stream)
+def _memory_of(stream, make, *args, **kwargs):
+    """make(...) with the memory of the stream that the call runs on: nothing that another stream still uses."""
+    if stream is None:
+        return make(*args, **kwargs)
+    with torch.cuda.stream(stream):
+        return make(*args, **kwargs)
 
 
 _TYPE = {torch.float32: 0, torch.bfloat16: 1}
@@ -129,9 +128,11 @@ def _rows(t, heads, dim, dtype, dev):
     """Pointer and row stride of packed rows [rows, heads, dim]; the rows may be slices of wider ones."""
     assert t.dtype is dtype and t.dim() == 3, f"expected [rows, {heads}, {dim}] of {dtype}, got {tuple(t.shape)} of {t.dtype}"
     rows, h, d = t.shape
-    row, head, one = t.stride()
     assert h == heads and d == dim, f"expected [rows, {heads}, {dim}], got {tuple(t.shape)}"
     assert t.get_device() == dev, "packed rows must be on the current device"
+    if t.is_contiguous():
+        return t.data_ptr(), heads * dim
+    row, head, one = t.stride()
     assert one == 1 and (head == dim or heads == 1), "the heads of a row must be next to each other"
     return t.data_ptr(), row if rows > 1 else heads * dim
 
@@ -378,8 +379,7 @@ class Tsdp:
     def tsdp_cache_read(self, cache, row_ptr, start, rows, dtype, out=None, stream=None):
         """Positions start[b] .. of every environment as packed rows (k, v); out: such a pair to write into."""
         if out is None:
-            with _memory_on(stream):
-                out = row_ptr.new_empty((2, rows, cache.kv_heads, cache.head_dim), dtype=dtype).unbind()
+            out = _memory_of(stream, row_ptr.new_empty, (2, rows, cache.kv_heads, cache.head_dim), dtype=dtype).unbind()
         assert out[0].dtype is dtype and out[0].shape[0] == rows, "out must hold `rows` rows of the given type"
         self._cache_rows(self.lib.tsdp_cache_read, cache, row_ptr, start, out[0], out[1], stream)
         return out
@@ -398,8 +398,7 @@ class Tsdp:
         (rows, heads, dim), (k_rows, kv, _) = q.shape, k.shape
         assert dtype in _TYPE and v.shape[0] == k_rows, "q, k and v must be of one type, float32 or bfloat16, and k and v alike"
         if out is None:
-            with _memory_on(stream):
-                out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            out = _memory_of(stream, torch.empty_like, q, memory_format=torch.contiguous_format)
         assert out.shape[0] == rows, "out must be alike q"
         qp, q_row = _rows(q, heads, dim, dtype, dev)
         kp, k_row = _rows(k, kv, dim, dtype, dev)
@@ -419,7 +418,7 @@ class Tsdp:
         n = self.lib.tsdp_attend_scratch(h, cache.B if B is None else B, tokens, max_len)
         if n < 0:
             raise TsdpError(int(n), "tsdp_attend_scratch rejected the sizes")
-        return torch.empty(n, dtype=torch.uint8, device=cache.k.device) if n else None
+        return cache.k.new_empty(n, dtype=torch.uint8) if n else None
 
     def tsdp_attend_paged(self, q, cache, length, max_len, *, tokens=1, causal=True, scale=None, out_dtype=None, out=None, lse=None,
                           scratch=None, stream=None):
@@ -431,13 +430,11 @@ class Tsdp:
         assert cache.device == dev, "the cache must be on the current device"
         assert dtype in _TYPE and rows == B * tokens and dim == cache.head_dim, "q must be [B * tokens, q_heads, head_dim], float32 or bfloat16"
         if out is None:
-            with _memory_on(stream):
-                out = torch.empty_like(q, dtype=out_dtype, memory_format=torch.contiguous_format)
+            out = _memory_of(stream, torch.empty_like, q, dtype=out_dtype, memory_format=torch.contiguous_format)
         assert out.dtype in _TYPE and out.shape[0] == rows and out_dtype in (None, out.dtype), "out must be alike q, float32 or bfloat16"
         assert scratch is None or scratch.get_device() == dev, "scratch must be on the current device"
         if scratch is None:
-            with _memory_on(stream):
-                scratch = self.alloc_scratch(cache, heads, tokens, max_len, B)
+            scratch = _memory_of(stream, self.alloc_scratch, cache, heads, tokens, max_len, B)
         qp, q_row = _rows(q, heads, dim, dtype, dev)
         op, out_row = _rows(out, heads, dim, out.dtype, dev)
         rc = self.lib.tsdp_attend_paged(self.ctx, TsdpHeads(_TYPE[dtype], heads, cache.kv_heads, dim, 1 if causal else 0, dim ** -0.5 if scale is None else scale),
