@@ -70,8 +70,8 @@ int cache_rows(tsdp_ctx* c, const tsdp_kv_cache* cache, int B, int R_cap, int ty
 
 template <int TQ>
 dim3 prompt_grid(PromptArgs& a) {
-  a.slots = (int)prompt_slots(a.q_cap, a.B, TQ);
-  return dim3((unsigned)((int64_t)a.slots * a.heads));
+  a.slots = (int)prompt_slots(a.q_cap, a.group, a.B, TQ);
+  return dim3((unsigned)((int64_t)a.slots * a.kv_heads));
 }
 
 template <int D>
@@ -143,7 +143,7 @@ int tsdp_attend_prompt(tsdp_ctx* c, const tsdp_heads* h, int B, int q_cap, int k
   if (B == 0 || q_cap == 0) return TSDP_OK;
   if (int rc = check_device(c)) return rc;
   PromptArgs a{};
-  a.B = B; a.q_cap = q_cap; a.k_cap = k_cap; a.heads = h->q_heads; a.kv_heads = h->kv_heads; a.causal = h->causal;
+  a.B = B; a.q_cap = q_cap; a.k_cap = k_cap; a.heads = h->q_heads; a.kv_heads = h->kv_heads; a.group = h->q_heads / h->kv_heads; a.causal = h->causal;
   a.c = h->scale * LOG2E; a.q_ptr = d_q_ptr; a.k_ptr = d_k_ptr ? d_k_ptr : d_q_ptr;
   a.q = d_q; a.k = d_k; a.v = d_v; a.out = d_out; a.q_row = q_row; a.k_row = k_row; a.v_row = v_row; a.out_row = out_row;
   a.lse = d_lse; a.status = ctx_status(c);

@@ -76,7 +76,7 @@ inline Fault prompt_fault(const tsdp_heads* h, int B, int q_cap, int k_cap, cons
   Fault f = heads_fault(h);
   if (f.code) return f;
   if (B < 0 || q_cap < 0 || k_cap < 0) return {TSDP_E_SHAPE, "B, q_cap and k_cap must not be negative"};
-  if (h->q_heads * prompt_slots(q_cap, B, 64) > MOST_GRID || k_cap > MOST_LENGTH) return {TSDP_E_SHAPE, "too many rows times heads for one launch"};
+  if (h->kv_heads * prompt_slots(q_cap, h->q_heads / h->kv_heads, B, 64) > MOST_GRID || k_cap > MOST_LENGTH) return {TSDP_E_SHAPE, "too many rows times heads for one launch"};
   if (B == 0 || q_cap == 0) return NO_FAULT;
   if (!q_ptr) return {TSDP_E_INVAL, "null row table"};
   if (!k_ptr && k_cap != q_cap) return {TSDP_E_INVAL, "without a row table of the keys k_cap must equal q_cap"};

@@ -89,7 +89,7 @@ inline int64_t cache_blocks(int64_t rows, int kv_heads, int head_dim) {
   const int64_t n = 4 * rows_per_wave(kv_heads, head_dim);
   return (rows + n - 1) / n;
 }
-inline int64_t prompt_slots(int64_t rows, int64_t B, int tq) { return rows / tq + B; }
+inline int64_t prompt_slots(int64_t rows, int group, int64_t B, int tq) { return rows * group / tq + B; }   // columns: rows x heads of a group
 inline int64_t paged_blocks(int64_t bk, int cols) { return cols <= 16 ? bk : bk * ((cols + 63) / 64); }
 inline int64_t join_blocks(int64_t bk, int cols, int chunks, int head_dim) {
   const int64_t columns = bk * cols, per = join_columns(head_dim);

@@ -299,7 +299,7 @@ __device__ __forceinline__ void wide_out(const W& w, __bf16* out, float l, int g
   }
 }
 
-// PAGED: the columns of a kv head over a chunk of the cache; otherwise the queries of a head over their sequence's rows.
+// PAGED: the columns of a kv head over a chunk of the cache; otherwise those of a sequence over its rows.
 // Waves a SIMD: as many as registers allow; heads of 64 over the cache are held to the 128 of four (64 queries of 32 sequences of 4000
 // tokens, 12 / 4 heads in 8 bits, the call: 79.7 us, 83.2 with the 130 of three), but for queries of three parts, which need 146.
 template <bool PAGED> constexpr int WIDE_GROUPS = PAGED ? 1 : 2;
@@ -354,10 +354,11 @@ __global__ __launch_bounds__(256 * WIDE_GROUPS<PAGED>, (D == 128 ? 2 : PAGED && 
   } else {
     if (!prompt_tile<COLS>(a, t)) return;
     kvh = t.kv_head; b = t.b;
-    tiles = (seen(min(t.i0 + COLS, t.nq) - 1, t.nq, t.nk, a.causal) + KT - 1) / KT;
-    plain = seen(t.i0, t.nq, t.nk, a.causal) / KT;
+    G = a.group;
+    tiles = (seen((min(t.i0 + COLS, t.columns) - 1) / G, t.nq, t.nk, a.causal) + KT - 1) / KT;
+    plain = seen(t.i0 / G, t.nq, t.nk, a.causal) / KT;
     col = t.i0 + 16 * wave + r;
-    mine = col < t.nq ? seen(col, t.nq, t.nk, a.causal) : 0;
+    mine = col < t.columns ? seen(col / G, t.nq, t.nk, a.causal) : 0;
   }
 
   constexpr int AHEAD = W::AHEAD;
@@ -397,7 +398,8 @@ __global__ __launch_bounds__(256 * WIDE_GROUPS<PAGED>, (D == 128 ? 2 : PAGED && 
     const int at = min(col, a.cols - 1);
     w.start(a.q, ((int64_t)b * a.tokens + at / G) * a.q_row + (kvh * G + at % G) * D, g);
   } else {
-    w.start(a.q, (int64_t)(t.q_lo + min(col, t.nq - 1)) * a.q_row + t.head * D, g);
+    const int at = min(col, t.columns - 1);
+    w.start(a.q, (int64_t)(t.q_lo + at / G) * a.q_row + (kvh * G + at % G) * D, g);
   }
   w.clear();
 
@@ -544,9 +546,9 @@ __global__ __launch_bounds__(256 * WIDE_GROUPS<PAGED>, (D == 128 ? 2 : PAGED && 
       return;
     }
   } else {
-    if (col >= t.nq) return;
-    head = t.head;
-    row = t.q_lo + col;
+    if (col >= t.columns) return;
+    head = kvh * G + col % G;
+    row = t.q_lo + col / G;
   }
   wide_out(w, static_cast<Out*>(a.out) + row * a.out_row + head * D, l, g);
   if (a.lse && g == 0) a.lse[row * a.heads + head] = (w.m + __builtin_amdgcn_logf(l)) * LN2;
