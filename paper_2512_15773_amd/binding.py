@@ -413,8 +413,9 @@ class Tsdp:
         return out
 
     def alloc_scratch(self, cache, q_heads, tokens, max_len, B=None):
-        """Scratch of tsdp_attend_paged for B environments (default: as many as the page table has), uint8, or None."""
-        h = TsdpHeads(0, q_heads, cache.kv_heads, cache.head_dim, 1, 1.0)
+        """Scratch of tsdp_attend_paged for B environments (default: as many as the page table has), uint8, or None.  A cache of 8
+        bits: for queries of either type (fp32 ones need the most)."""
+        h = TsdpHeads(1 if cache.c.type == 1 else 0, q_heads, cache.kv_heads, cache.head_dim, 1, 1.0)
         n = self.lib.tsdp_attend_scratch(h, cache.B if B is None else B, tokens, max_len)
         if n < 0:
             raise TsdpError(int(n), "tsdp_attend_scratch rejected the sizes")

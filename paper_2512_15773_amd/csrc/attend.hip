@@ -171,8 +171,8 @@ int tsdp_attend_paged(tsdp_ctx* c, const tsdp_heads* h, const tsdp_kv_cache* cac
   if (int rc = check_device(c)) return rc;
   PagedArgs a{};
   a.cache = view_of(cache);
-  a.B = B; a.heads = h->q_heads; a.tokens = tokens; a.cols = tokens * (h->q_heads / h->kv_heads); a.max_len = max_len;
-  a.max_chunks = std::max(1, most_chunks(max_len, a.cols)); a.causal = h->causal; a.c = h->scale * LOG2E;
+  a.B = B; a.heads = h->q_heads; a.tokens = tokens; a.cols = tokens * (h->q_heads / h->kv_heads); a.max_len = max_len; a.fp32 = h->type == 0;
+  a.max_chunks = std::max(1, most_chunks(max_len, a.cols, a.fp32)); a.causal = h->causal; a.c = h->scale * LOG2E;
   a.len = d_len; a.q = d_q; a.out = d_out; a.q_row = q_row; a.out_row = out_row; a.lse = d_lse; a.status = ctx_status(c);
   a.part = static_cast<float*>(d_scratch);
   a.part_ml = a.part + (int64_t)B * h->kv_heads * a.cols * a.max_chunks * h->head_dim;

@@ -90,7 +90,7 @@ inline Fault prompt_fault(const tsdp_heads* h, int B, int q_cap, int k_cap, cons
 // scratch of one call in bytes, -1 where the sizes are outside what one launch takes (heads: checked)
 inline int64_t scratch_bytes(const tsdp_heads* h, int B, int tokens, int max_len) {
   if (B < 0 || tokens < 1 || tokens > MOST_TOKENS || max_len < 0) return -1;
-  const int cols = tokens * (h->q_heads / h->kv_heads), n = most_chunks(max_len, cols);
+  const int cols = tokens * (h->q_heads / h->kv_heads), n = most_chunks(max_len, cols, h->type == 0);
   const int64_t bk = (int64_t)B * h->kv_heads;
   if (n > MOST_GRID_Y || paged_blocks(bk, cols) > MOST_GRID || join_blocks(bk, cols, n, h->head_dim) > MOST_GRID) return -1;
   return n <= 1 ? 0 : (int64_t)B * h->kv_heads * cols * n * (h->head_dim + 2) * 4;

@@ -22,7 +22,7 @@ namespace tsdp {
 
 struct PagedArgs {
   CacheView cache;
-  int B, heads, tokens, cols, max_len, max_chunks, causal;   // cols = tokens * heads / kv_heads
+  int B, heads, tokens, cols, max_len, max_chunks, causal, fp32;   // cols = tokens * heads / kv_heads; fp32: type of the queries
   float c;
   const int32_t* len;
   const void* q; void* out;
@@ -361,7 +361,7 @@ __global__ __launch_bounds__(256, 2) void k_paged(PagedArgs a) {
   __shared__ float ml_lds[4][16][2];
   const int kv = a.cache.kv_heads, kvh = blockIdx.x % kv, b = blockIdx.x / kv, chunk = blockIdx.y;
   const int len = paged_len(a, b);
-  const int shift = chunk_shift(len, a.cols), chunks = chunks_of(len, a.cols);
+  const int shift = chunk_shift(len, a.cols, a.fp32), chunks = chunks_of(len, a.cols, a.fp32);
   if (chunk > 0 && chunk >= chunks) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
   const int G = a.heads / kv, per_wave = 1 << (shift - 2);       // keys of a wave
@@ -550,7 +550,7 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedArgs a) {
   const int64_t column = FEW ? (int64_t)blockIdx.x * join_columns(D) + threadIdx.x / Join::LANES : blockIdx.x;
   if (column >= (int64_t)a.B * kv * a.cols) return;
   const int col = (int)(column % a.cols), bk = (int)(column / a.cols), b = bk / kv;
-  const int chunks = chunks_of(paged_len(a, b), a.cols);
+  const int chunks = chunks_of(paged_len(a, b), a.cols, a.fp32);
   if (chunks <= 1) return;
   const int64_t at = column * a.max_chunks;
   Join j;

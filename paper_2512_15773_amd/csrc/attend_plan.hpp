@@ -51,26 +51,28 @@ TSDP_HD int seen(int i, int nq, int nk, bool causal) {
 }
 
 // Chunk of a sequence that one workgroup of the paged kernel takes, from the sequence's own length and the columns
-// (queries x heads of a group) alone, so that a result does not depend on the batch around it.  Short chunks spread one short
+// (queries x heads of a group) and type alone, so that a result does not depend on the batch around it.  Short chunks spread one short
 // sequence over the chip (700 keys in fp32, 8 heads of 64: 8.0 us in chunks of 256, 11.2 in chunks of 512, without the join);
 // long ones leave fewer partial results (16 sequences of 4096, 32 / 8 heads of 128 in 8 bits, the call: 29.8 us in chunks of
-// 512, 34.2 in chunks of 256).
-TSDP_HD int chunk_shift(int len, int cols) {
-  int s = cols <= 16 ? 8 : 10;
+// 512, 34.2 in chunks of 256).  Many columns take longer for a key, with queries in fp32 twice as long again (32 sequences of 8000,
+// 64 queries, 12 / 4 heads of 64 in 8 bits: 157 us in chunks of 1024, 178 in chunks of 512; in fp32, 32 of 1000, 12 / 3 heads of 64:
+// 56.1 in chunks of 512, 67.4 in one of 1024; 32 of 4000: 203 in both; 32 of 4000 with 8 bits held: 103 and 94, 5 of 3000: 26.7 and 29.6).
+TSDP_HD int chunk_shift(int len, int cols, bool fp32 = false) {
+  int s = cols <= 16 ? 8 : fp32 ? 9 : 10;
   if (len > (1 << 10) && s < 9) s = 9;
   if (len > (1 << 14) && s < 10) s = 10;
   if (len > (1 << 16) && cols <= 16) s = 11;
   return s;
 }
-TSDP_HD int chunks_of(int len, int cols) {
-  const int s = chunk_shift(len, cols);
+TSDP_HD int chunks_of(int len, int cols, bool fp32 = false) {
+  const int s = chunk_shift(len, cols, fp32);
   return (int)(((long)len + (1L << s) - 1) >> s);
 }
 // the most chunks that a length of at most max_len has
-inline int most_chunks(int max_len, int cols) {
-  int n = chunks_of(max_len, cols);
+inline int most_chunks(int max_len, int cols, bool fp32 = false) {
+  int n = chunks_of(max_len, cols, fp32);
   for (int at : {1 << 10, 1 << 14, 1 << 16})     // where chunks grow
-    if (max_len > at && chunks_of(at, cols) > n) n = chunks_of(at, cols);
+    if (max_len > at && chunks_of(at, cols, fp32) > n) n = chunks_of(at, cols, fp32);
   return n;
 }
 

@@ -335,8 +335,8 @@ __global__ __launch_bounds__(256 * WIDE_GROUPS<PAGED>, (D == 128 ? 2 : PAGED && 
     const int col0 = (rest % ct) * COLS;
     b = rest / ct;
     len = paged_len(a, b);
-    const int shift = chunk_shift(len, a.cols);
-    chunks = chunks_of(len, a.cols);
+    const int shift = chunk_shift(len, a.cols, a.fp32);
+    chunks = chunks_of(len, a.cols, a.fp32);
     if (chunk > 0 && chunk >= chunks) return;
     G = a.heads / kv;
     lo = (long)chunk << shift;

@@ -22,9 +22,9 @@ int page(const int32_t* table, int pages, int columns, int b, long col) {
 int64_t row(int kv, int shift, int page, int head, int token) { CacheView c{}; c.kv_heads = kv; c.page_shift = shift; return pool_row(c, page, head, token); }
 void rows(const int32_t* ptr, int b, int cap, int* lo, int* hi) { rows_of(ptr, b, cap, *lo, *hi); }
 int sees(int i, int nq, int nk, int causal) { return seen(i, nq, nk, causal != 0); }
-int chunks(int len, int cols) { return chunks_of(len, cols); }
-int chunk(int len, int cols) { return 1 << chunk_shift(len, cols); }
-int most(int max_len, int cols) { return most_chunks(max_len, cols); }
+int chunks(int len, int cols, int fp32) { return chunks_of(len, cols, fp32 != 0); }
+int chunk(int len, int cols, int fp32) { return 1 << chunk_shift(len, cols, fp32 != 0); }
+int most(int max_len, int cols, int fp32) { return most_chunks(max_len, cols, fp32 != 0); }
 int refuse_rows(const tsdp_kv_cache* c, int B, int R, int type, const int32_t* p, const int32_t* s, const void* k, int64_t kr, const void* v, int64_t vr) {
   return cache_rows_fault(c, B, R, type, p, s, k, kr, v, vr).code;
 }
@@ -91,18 +91,20 @@ def test_keys_that_a_query_sees(plan):
     assert plan.sees(0, 2 ** 31 - 1, 0, 1) == 0 and plan.sees(2 ** 31 - 2, 2 ** 31 - 1, 2 ** 31 - 1, 1) == 2 ** 31 - 1
 
 
-def test_chunks_cover_a_length_and_their_bound_holds(plan):
+@pytest.mark.parametrize("fp32", (0, 1))
+def test_chunks_cover_a_length_and_their_bound_holds(plan, fp32):
     rng = np.random.default_rng(0)
     for cols in (1, 8, 16, 17, 33, 64, 65, 1024):
         lens = [0, 1, 255, 256, 257, 1024, 1025, 16383, 16384, 16385, 65536, 65537, 131072] + rng.integers(0, 300000, 50).tolist()
         for n in lens:
-            c = plan.chunk(n, cols)
+            c = plan.chunk(n, cols, fp32)
             assert c >= 128 and c % 128 == 0                          # four waves of whole tiles
-            assert plan.chunks(n, cols) == -(-n // c)
+            assert c <= (2048 if cols <= 16 else 1024)                # 64 lanes hold the pages of 16 tokens each, of a wave or of all four
+            assert plan.chunks(n, cols, fp32) == -(-n // c)
         for most in lens:
-            bound = plan.most(most, cols)
+            bound = plan.most(most, cols, fp32)
             for n in [x for x in lens if x <= most] + [min(most, 1024), min(most, 16384), min(most, 65536)]:
-                assert plan.chunks(n, cols) <= bound, (n, most, cols)
+                assert plan.chunks(n, cols, fp32) <= bound, (n, most, cols)
 
 
 @pytest.mark.parametrize("tq", (32, 64, 128))
