@@ -324,7 +324,8 @@ int tsdp_cache_write(tsdp_ctx* ctx, const tsdp_kv_cache* cache, int B, int R_cap
 int tsdp_cache_read(tsdp_ctx* ctx, const tsdp_kv_cache* cache, int B, int R_cap, int type, const int32_t* d_row_ptr,
                     const int32_t* d_start, void* d_k, int64_t k_row, void* d_v, int64_t v_row, void* stream);
 
-/* Attention of whole prompts.  d_q [q_cap, q_heads, head_dim] with d_q_ptr[B+1], d_k / d_v [k_cap, kv_heads, head_dim] with
+/* Attention of whole prompts.  (A few queries behind a long history are tsdp_attend_paged's: here one workgroup takes all keys of
+ * a tile of them.)  d_q [q_cap, q_heads, head_dim] with d_q_ptr[B+1], d_k / d_v [k_cap, kv_heads, head_dim] with
  * d_k_ptr[B+1] (NULL: as the queries, and k_cap = q_cap).  out: d_out as d_q.  Scores, sums and outputs are accumulated in
  * fp32; with type 1 the weights are rounded to bf16 for their product with the values. */
 int tsdp_attend_prompt(tsdp_ctx* ctx, const tsdp_heads* heads, int B, int q_cap, int k_cap, const int32_t* d_q_ptr,

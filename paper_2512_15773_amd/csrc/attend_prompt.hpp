@@ -3,14 +3,14 @@
 //   o_i = sum_j p_ij v_j / sum_j p_ij,  p_ij = exp(scale <q_i, k_j> - m_i) over the keys that query i sees
 //
 // One pass over the keys with a running maximum m_i, sum and output (all fp32), so scores never leave the registers.  A wave
-// owns 32 queries of one head; the waves of a workgroup share the tiles of keys and values in LDS.  Both products are taken
+// owns 32 columns (a query of one head each); the waves of a workgroup share the tiles of keys and values in LDS.  Both products are taken
 // transposed, S^T = K Q^T and O^T = V^T P^T: a lane then holds scores of one query only (column l % 32), so the softmax
 // needs one exchange between the wave's halves per tile, and the accumulator layout of S^T is the operand layout of P^T as it
 // is, up to the order of the keys, which the value operand follows: P stays in registers.
 //
-// Measured: two prompts of 5003..8192 tokens, 32 / 8 heads of 128, 890 us = 1.06 PFLOP/s (a large library product: 1.19 to 1.36; the
+// Measured: two prompts of 5003..8192 tokens, 32 / 8 heads of 128, 880 us = 1.08 PFLOP/s (a large library product: 1.19 to 1.36; the
 // matrix pipe is busy 55 % of the time, the exponentials and their conversion fill the vector pipe meanwhile); 16 chunks of
-// 65..257 queries behind 2000 tokens, 16 / 4 heads of 128, 67 us = 0.67 PFLOP/s (few workgroups, of unequal length); 256 prompts of 1..191
+// 65..257 queries behind 2000 tokens, 16 / 4 heads of 128, 63 us = 0.71 PFLOP/s (few workgroups, of unequal length); 256 prompts of 1..191
 // tokens, 8 heads of 64, 36 us = 2.8 TB/s (each is a chain of look-up, loads, two to three tiles and stores).
 #pragma once
 #include "attend_common.hpp"
@@ -28,10 +28,14 @@ struct PromptArgs {
   int32_t* status;
 };
 
+// (most calls have no group: the division takes 1 of 37 us of 256 short prompts)
+__device__ __forceinline__ int query_of(int column, int group) { return group == 1 ? column : column / group; }
+
 // The tile of a workgroup: TQ columns of one kv head, a column being a query of one of the heads that share its keys (heads of a query
-// next to each other), so that short sequences fill it with all of them (180 prompts of 5 tokens, 32 / 4 heads of 128: 16.3 us in bf16,
-// 64.4 with a workgroup a head; in fp32 35.3 and 161; 32 of 300, 32 / 8 heads of 128 in bf16: 67.7 and 82.7).  Sequence b owns the slots from G q_ptr[b] / TQ + b on, G the heads of a group, which no other
-// does since floor(x) + ceil(n) <= floor(x + n) + 1.  Late tiles of late sequences come first: causal ones have the most keys.
+// next to each other), so that short sequences fill it with all of them (180 prompts of 5 tokens, 32 / 4 heads of 128: 16.3 us in
+// bf16, 64.4 with a workgroup a head; in fp32 35.3 and 161; 32 of 300, 32 / 8 heads of 128 in bf16: 67.7 and 82.7).  With G heads in
+// a group, sequence b owns the slots from G q_ptr[b] / TQ + b on, which no other does since floor(x) + ceil(n) <= floor(x + n) + 1.
+// Late tiles of late sequences come first: causal ones have the most keys.
 struct PromptTile { int b, kv_head, q_lo, nq, i0, columns, k_lo, nk; };
 template <int TQ>
 __device__ __forceinline__ bool prompt_tile(const PromptArgs& a, PromptTile& t) {
@@ -78,7 +82,7 @@ __device__ __forceinline__ void wait_loads() {
   asm volatile("" ::: "memory");
 }
 
-// bf16.  A wave owns 32 queries.  Keys go by 32 (half a tile) through three stages that do not depend on each other and are
+// bf16.  A wave owns 32 columns.  Keys go by 32 (half a tile) through three stages that do not depend on each other and are
 // issued into each other: scores of the next 32 keys (matrix pipe), softmax of these (vector pipe), product of the last 32
 // with their values (matrix pipe).  Key tiles are two buffers, and so are value tiles, a tile behind: one barrier a tile, in
 // its middle, where the tiles requested at the last one have landed and the oldest buffers are free again.  Each buffer is a
@@ -215,8 +219,8 @@ __global__ __launch_bounds__(NW * 64, WAVES) void k_prompt_bf16(PromptArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5;
   const int i0 = t.i0 + wave * 32, i = i0 + col, G = a.group;  // the wave's first column, this lane's
-  const int query = min(i, t.columns - 1) / G, head = t.kv_head * G + min(i, t.columns - 1) % G;
-  const auto sees = [&](int column) { return seen(column / G, t.nq, t.nk, a.causal); };
+  const int query = query_of(min(i, t.columns - 1), G), head = t.kv_head * G + min(i, t.columns - 1) - query * G;
+  const auto sees = [&](int column) { return seen(query_of(column, G), t.nq, t.nk, a.causal); };
   // tiles that every column of the workgroup sees in full, and that some column sees
   const int full = OVERLAP ? sees(t.i0) / KT : 0;
   const int tiles = (sees(min(t.i0 + C::TQ, t.columns) - 1) + KT - 1) / KT;

@@ -3,7 +3,7 @@
 //
 // A workgroup takes 64 columns and all keys of them (of its chunk), 32 keys at a time: they are loaded into registers some tiles
 // ahead, turned into bf16 once for all columns and put into LDS; each of four waves owns 16 columns.  Prompts have two such groups
-// of waves, which take tiles in turns and join at the end: half the way from the first key to the last (71 -> 64 us for four prompts
+// of waves, which take tiles in turns and join at the end: half the way from the first key to the last (64 us, 71 with one, for four prompts
 // of 301..1501 tokens, 8 heads of 64; over the cache, whose chunks are short, one group is faster by 14 % on ragged lengths).  fp32 becomes
 // three bf16 parts that add up to it to 2^-24, and a product of fp32 six products of parts (what is left out is 2^-25 of it each): 6 passes of
 // the bf16 matrix pipe take 3/8 of the time of one of the fp32 pipe.  8 bits are one part, their scale included.  Weights are three parts
@@ -12,7 +12,7 @@
 // Bound by the vector and LDS pipes of workgroups that run for different times (ragged lengths), not by memory: 64 queries of 32
 // sequences of 501..4000 tokens, 12 / 4 heads of 64 in 8 bits, outputs in fp32: 60.5 us = 240 TFLOP/s of the two products (each weight is
 // multiplied in three parts; vector pipe busy 40 %, 1.8 of 4 waves a SIMD resident on average); the fp32 prompts
-// above: 64 us = 87 TFLOP/s (matrix 23 %, vector 39 %).
+// above, now 61 us = 91 TFLOP/s (matrix 22 %, vector 37 %).
 //
 // The operand layouts are those of the narrow kernel: S^T = K Q^T, O^T = V^T P^T in tiles of 16, P in registers throughout.
 // The maximum is that of the first keys, as everywhere; a rise is noticed from the sums, and the workgroup starts over with
@@ -355,10 +355,10 @@ __global__ __launch_bounds__(256 * WIDE_GROUPS<PAGED>, (D == 128 ? 2 : PAGED && 
     if (!prompt_tile<COLS>(a, t)) return;
     kvh = t.kv_head; b = t.b;
     G = a.group;
-    tiles = (seen((min(t.i0 + COLS, t.columns) - 1) / G, t.nq, t.nk, a.causal) + KT - 1) / KT;
-    plain = seen(t.i0 / G, t.nq, t.nk, a.causal) / KT;
+    tiles = (seen(query_of(min(t.i0 + COLS, t.columns) - 1, G), t.nq, t.nk, a.causal) + KT - 1) / KT;
+    plain = seen(query_of(t.i0, G), t.nq, t.nk, a.causal) / KT;
     col = t.i0 + 16 * wave + r;
-    mine = col < t.columns ? seen(col / G, t.nq, t.nk, a.causal) : 0;
+    mine = col < t.columns ? seen(query_of(col, G), t.nq, t.nk, a.causal) : 0;
   }
 
   constexpr int AHEAD = W::AHEAD;
@@ -399,7 +399,8 @@ __global__ __launch_bounds__(256 * WIDE_GROUPS<PAGED>, (D == 128 ? 2 : PAGED && 
     w.start(a.q, ((int64_t)b * a.tokens + at / G) * a.q_row + (kvh * G + at % G) * D, g);
   } else {
     const int at = min(col, t.columns - 1);
-    w.start(a.q, (int64_t)(t.q_lo + at / G) * a.q_row + (kvh * G + at % G) * D, g);
+    const int query = query_of(at, G);
+    w.start(a.q, (int64_t)(t.q_lo + query) * a.q_row + (kvh * G + at - query * G) * D, g);
   }
   w.clear();
 
@@ -547,8 +548,9 @@ __global__ __launch_bounds__(256 * WIDE_GROUPS<PAGED>, (D == 128 ? 2 : PAGED && 
     }
   } else {
     if (col >= t.columns) return;
-    head = kvh * G + col % G;
-    row = t.q_lo + col / G;
+    const int query = query_of(col, G);
+    head = kvh * G + col - query * G;
+    row = t.q_lo + query;
   }
   wide_out(w, static_cast<Out*>(a.out) + row * a.out_row + head * D, l, g);
   if (a.lse && g == 0) a.lse[row * a.heads + head] = (w.m + __builtin_amdgcn_logf(l)) * LN2;
