@@ -108,11 +108,13 @@ def test_chunks_cover_a_length_and_their_bound_holds(plan, fp32):
 
 
 @pytest.mark.parametrize("tq", (32, 64, 128))
-def test_every_query_has_one_slot(tq):
-    """The rule by which a workgroup of the prompt kernel finds its rows: sequence b owns slots ptr[b] / tq + b and on."""
+@pytest.mark.parametrize("group", (1, 3, 8))
+def test_every_query_has_one_slot(tq, group):
+    """The rule by which a workgroup of the prompt kernel finds its columns (queries x heads of a group): sequence b owns slots
+    group * ptr[b] / tq + b and on."""
     rng = np.random.default_rng(tq)
     for _ in range(200):
-        n = rng.integers(0, 300, rng.integers(1, 70)) * rng.integers(0, 2)
+        n = group * (rng.integers(0, 300, rng.integers(1, 70)) * rng.integers(0, 2))
         ptr = np.concatenate([[0], np.cumsum(n)])
         B, slots = len(n), int(ptr[-1]) // tq + len(n)
         first = ptr[:-1] // tq + np.arange(B)
