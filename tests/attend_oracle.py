@@ -28,7 +28,7 @@ def attend(q, k, v, scale, causal):
 def bound(out, mean, size, dim, n, out_type, weights):
     """Elementwise error bound.  weights: relative rounding of a weight for its product with the values.  A score is a sum of dim
     products in fp32 (dim + 4 roundings of sums as large as `size`, among them the scale's), its exponential doubles nothing but
-    adds a few roundings and that of its argument (the score, and up to 8 of a running maximum left behind); sums over n keys
+    adds a few roundings and that of its argument (the distance to a maximum, at most twice the largest score); sums over n keys
     round once per key and join; the quotient and the output round once each."""
     u = 2.0 ** -24
     weight = weights + 2 * ((dim + 4) * u * size + 2 * u * (size + 12)) + 8 * u
